@@ -290,9 +290,13 @@ def _encode(x, noise, top):
     bits = x.view(torch.int32).view(-1, BLOCK)
     sign, bits = bits < 0, bits & 0x7FFFFFFF
     e = bits.amax(1, keepdim=True) >> 23
-    code = ((bits + (noise.view(-1, BLOCK) << 4)) >> 20) - ((e + 1) * 8 - top)
+    held = (bits + (noise.view(-1, BLOCK) << 4)) >> 20
+    first = (e + 1) * 8 - top
+    if top == 127:
+        code = torch.where(held > 0, torch.clamp(held - first, min=0), 0)
+    else:
+        code = torch.where(bits > 0, torch.clamp(torch.clamp(held, min=1) - first, min=1), 0)
     code = torch.minimum(code, top - (e == 254).int())
-    code = torch.clamp(code, min=0) if top == 127 else torch.where(bits > 0, torch.clamp(code, min=1), 0)
     if top == 127:
         code = code + 128 * (sign & (code > 0))
     return torch.where(e == 255, 0, code).to(torch.uint8).reshape(-1), e.reshape(-1).to(torch.uint8)
