@@ -2,6 +2,7 @@
 // kernels of one layer are enqueued.  No allocation, no synchronisation.
 #include "../../include/gswa.h"
 #include "common.h"
+#include "args.h"
 #include "staged_kernels.h"
 #include "fused.h"
 #include "window_layer.h"
@@ -125,15 +126,6 @@ size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 template <typename... P> bool aligned16(P... p) { return (((reinterpret_cast<uintptr_t>(p)) | ...) & 15) == 0; }
 
 size_t elem_size(const gswa_desc *d) { return d->dtype == GSWA_F32 ? 4 : 2; }
-
-// A device buffer as a byte range, for the overlap rules of the entry points.
-struct Range {
-    uintptr_t lo, hi;
-    Range(const void *p, size_t bytes) : lo(reinterpret_cast<uintptr_t>(p)), hi(lo + (p ? bytes : 0)) {}
-};
-bool overlap(const Range &a, const Range &b) { return a.lo < b.hi && b.lo < a.hi; }
-// true when `out` shares a byte with any of the others
-template <typename... R> bool overlaps_any(const Range &out, const R &...others) { return (overlap(out, others) || ...); }
 
 struct Sizes {
     size_t saved, qkv, fwd_ws, bwd_ws;

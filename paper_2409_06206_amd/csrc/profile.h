@@ -46,6 +46,16 @@ enum KernelId {
     K_WINDOW_BWD,    // its backward
     K_LAYER_FWD,     // a whole layer (Eq. 4-5), one workgroup per window
     K_LAYER_BWD,     // its adjoint
+    K_LNORM_FWD,     // LayerNorm of rows (lnorm.h), residual added first
+    K_LNORM_BWD,     // its adjoint, and partial sums of gamma's and beta's gradient
+    K_LNORM_SUM,     // those sums
+    K_RELPOS_FWD,    // relative position bias from buckets (relpos.h)
+    K_RELPOS_BWD,    // partial sums of its gradient
+    K_RELPOS_SUM,    // those sums
+    K_ADAMW_PLAN,    // places of the tensors of a step (adamw.h), laid out for the device
+    K_ADAMW_NORM,    // norm of all gradients
+    K_ADAMW_STEP,    // one step over all tensors
+    K_ADAMW_UNPACK,  // 8-bit states as bf16
     K_COUNT
 };
 

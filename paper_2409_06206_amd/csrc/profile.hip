@@ -28,7 +28,9 @@ const char *kernel_name(int id)
                                          "wproj_grad", "attn_core_fwd", "attn_core_bwd", "qkv+dO_linear", "window_fwd",
                                          "ln_fwd", "ln_bwd", "gelu_fwd", "gelu_bwd", "fc1_linear", "fc2_linear",
                                          "fc_dlinear", "fc_wgrad", "mlp_fwd", "mlp_bwd", "mlp_pack", "mlp_reduce", "ln_fwd+mlp_reduce",
-                                         "wide_attn_bwd", "wide_qkv_grad", "window_attn_fwd", "window_bwd", "layer_fwd", "layer_bwd"};
+                                         "wide_attn_bwd", "wide_qkv_grad", "window_attn_fwd", "window_bwd", "layer_fwd", "layer_bwd",
+                                         "lnorm_fwd", "lnorm_bwd", "lnorm_sum", "relpos_fwd", "relpos_bwd", "relpos_sum",
+                                         "adamw_plan", "adamw_norm", "adamw_step", "adamw_unpack"};
     return (id >= 0 && id < K_COUNT) ? names[id] : "?";
 }
 
