@@ -32,7 +32,7 @@ enum {
 
 typedef struct lnorm_desc {
     int64_t rows;      /* > 0                                                                            */
-    int32_t C;         /* values per row, 1 .. 32768 (GSWA_BF16) or 16384 (GSWA_F32)                     */
+    int32_t C;         /* values per row, 1 .. 16384                                                     */
     int32_t dtype;     /* GSWA_F32 or GSWA_BF16: x, residual, gamma, beta, y, sum, dy, dsum, dx          */
     float eps;         /* >= 0                                                                           */
     uint32_t flags;    /* LNORM_ACCUM_WGRAD                                                              */

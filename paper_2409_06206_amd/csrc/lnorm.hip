@@ -1,134 +1,393 @@
 // LayerNorm of rows, forward and backward (lnorm.h): the kernels and the C ABI.
+//
+// Both passes are bound by memory: about ten operations an element against 4 to 14 bytes.  So a row is read once, stays in the registers
+// of L lanes (P vectors of 16 bytes each), and all of a row's sums are formed there: the mean, then the squares of the distances from it (in a second
+// round, so that a mean far from zero costs the variance no digits).
 #include "../../include/lnorm.h"
 #include "args.h"
 #include "common.h"
 #include "mfma.h"
 #include "profile.h"
 
+#include <type_traits>
+
 namespace gswa {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kSlices = 64; // of the rows, in the sums of the parameter gradients
+constexpr int kSumThreads = 1024, kSumColumns = 32;
+constexpr int N_MAX = 3; // sums of a row that are formed at once
 
 struct Args {
     const void *x, *residual, *gamma, *beta, *dy, *dsum;
     void *y, *sum, *dx;
-    float2 *stats;  // backward: mean and 1 / sqrt(var + eps) of every row
-    float *part;    // backward: [kSlices][2 C]
+    float *part;    // backward: [workgroups][2 C], null where no parameter gradients are wanted
     float *dgamma, *dbeta;
     long rows, ldx, ldy, ldr;
-    int C, accumulate;
+    int C, accumulate, parts;
     float eps;
 };
 
-__device__ __forceinline__ float block_sum(float v, float *lds)
+// V values as they lie in memory; a row starts anywhere, so only the alignment of an element is promised (the wide loads and stores take any).
+template <typename T, int V> struct Raw {
+    typename std::conditional<V * sizeof(T) == 16, uint4, T>::type w;
+};
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load(const T *p)
 {
+    Raw<T, V> r;
+    __builtin_memcpy(&r.w, p, V * sizeof(T));
+    return r;
+}
+__device__ __forceinline__ void unpack(const Raw<bf16_t, 8> &r, float *f)
+{
+    f[0] = bf16_lo(r.w.x); f[1] = bf16_hi(r.w.x); f[2] = bf16_lo(r.w.y); f[3] = bf16_hi(r.w.y);
+    f[4] = bf16_lo(r.w.z); f[5] = bf16_hi(r.w.z); f[6] = bf16_lo(r.w.w); f[7] = bf16_hi(r.w.w);
+}
+__device__ __forceinline__ void unpack(const Raw<float, 4> &r, float *f)
+{
+    f[0] = __uint_as_float(r.w.x); f[1] = __uint_as_float(r.w.y); f[2] = __uint_as_float(r.w.z); f[3] = __uint_as_float(r.w.w);
+}
+template <typename T> __device__ __forceinline__ void unpack(const Raw<T, 1> &r, float *f) { f[0] = to_f32(r.w); }
+__device__ __forceinline__ Raw<bf16_t, 8> pack(const float *f, Raw<bf16_t, 8>)
+{
+    return {make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]))};
+}
+__device__ __forceinline__ Raw<float, 4> pack(const float *f, Raw<float, 4>)
+{
+    return {make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]))};
+}
+template <typename T> __device__ __forceinline__ Raw<T, 1> pack(const float *f, Raw<T, 1> r)
+{
+    from_f32(r.w, f[0]);
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store(T *p, const float *f)
+{
+    const Raw<T, V> r = pack(f, Raw<T, V>{});
+    __builtin_memcpy(p, &r.w, V * sizeof(T));
+}
+
+// The compiler may not carry what it unpacked from these over this point (it would hold a register for each value, where unpacking again is one
+// instruction).
+__device__ __forceinline__ void again(Raw<bf16_t, 8> &r) { asm volatile("" : "+v"(r.w.x), "+v"(r.w.y), "+v"(r.w.z), "+v"(r.w.w)); }
+__device__ __forceinline__ void again(Raw<float, 4> &r) { asm volatile("" : "+v"(r.w.x), "+v"(r.w.y), "+v"(r.w.z), "+v"(r.w.w)); }
+template <typename T> __device__ __forceinline__ void again(Raw<T, 1> &) {}
+
+// V ones or zeros where gamma or beta is not given: the loop over the rows has no branch for it
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> all(float v)
+{
+    float f[V];
 #pragma unroll
-    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    for (int i = 0; i < V; ++i) f[i] = v;
+    return pack(f, Raw<T, V>{});
 }
 
-// mean and 1 / sqrt(var + eps) of a row: the squares are of distances from the mean, in a second pass
-template <typename T> __device__ __forceinline__ float2 row_stats(const T *row, int C, float eps, float *lds)
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v)
 {
-    float s = 0.f, q = 0.f;
-    for (int c = threadIdx.x; c < C; c += kThreads) s += to_f32(row[c]);
-    const float mean = block_sum(s, lds) / (float)C;
-    for (int c = threadIdx.x; c < C; c += kThreads) {
-        const float d = to_f32(row[c]) - mean;
-        q += d * d;
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+// v_permlane16_swap(v, v) and v_permlane32_swap(v, v) leave v and its partner of the other row of 16 lanes, or half of the wavefront, in the two results
+__device__ __forceinline__ float rows_add(float v)
+{
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_add(float v)
+{
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// sum over groups of 8 to 64 lanes: pairs, quads, halves of a row of 16 lanes (a mirrored lane holds what the exchanged one holds), rows, halves
+template <int L> __device__ __forceinline__ float lanes_sum(float v)
+{
+    v = dpp_add<0xB1>(v);
+    v = dpp_add<0x4E>(v);
+    v = dpp_add<0x141>(v);
+    if constexpr (L >= 16) v = dpp_add<0x140>(v);
+    if constexpr (L >= 32) v = rows_add(v);
+    if constexpr (L >= 64) v = halves_add(v);
+    return v;
+}
+
+// The L lanes of a row, and what each holds of it: vector p of a lane is columns [column(p), column(p) + V).  The row's last vector ends
+// at column C: where C is no multiple of V it begins inside the one before it, whose columns it reads as well but does not own.  (So no load or store
+// is ever narrower than a vector; both lanes store the same values.)
+template <int L, int P, int V> struct Place {
+    static constexpr int kBlock = L > 256 ? L : 256, kGroups = kBlock / L, kWaves = kBlock / 64;
+    int C, lane;
+    __device__ __forceinline__ Place(int C_) : C(C_), lane((int)threadIdx.x % L) {}
+    __device__ __forceinline__ int column(int p) const
+    {
+        const int c = (p * L + lane) * V;
+        return c < C - V ? c : C - V;
     }
-    return make_float2(mean, rsqrtf(block_sum(q, lds) / (float)C + eps));
-}
-
-// One workgroup per row; a row is read again from the caches for each pass over it.
-template <typename T> __global__ __launch_bounds__(kThreads) void lnorm_fwd_kernel(Args a)
-{
-    __shared__ float lds[4];
-    const T *gamma = static_cast<const T *>(a.gamma), *beta = static_cast<const T *>(a.beta);
-    for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *u = static_cast<const T *>(a.x) + row * a.ldx;
-        if (a.residual) {
-            const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
-            T *s = static_cast<T *>(a.sum) + row * a.ldr;
-            for (int c = threadIdx.x; c < a.C; c += kThreads) from_f32(s[c], to_f32(u[c]) + to_f32(r[c]));
-            u = s; // (every thread reads back only what it wrote)
+    __device__ __forceinline__ bool any(int p) const { return p < P - 1 || (p * L + lane) * V < C; }
+    // whether element i of vector p is this lane's (P is the least that holds a row: only a lane's last vector can be short)
+    __device__ __forceinline__ bool own(int p, int i) const { return p < P - 1 || column(p) + i >= (p * L + lane) * V; }
+    template <typename T> __device__ __forceinline__ void fetch(const T *row, Raw<T, V> (&r)[P]) const
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) r[p] = load<T, V>(row + column(p));
+    }
+    // `without` throughout where there is no vector
+    template <typename T> __device__ __forceinline__ void fetch_or(const void *row, float without, Raw<T, V> (&r)[P]) const
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) r[p] = row ? load<T, V>(static_cast<const T *>(row) + column(p)) : all<T, V>(without);
+    }
+    template <typename T> __device__ __forceinline__ void put(T *row, const float (&f)[P * V]) const
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (any(p)) store<T, V>(row + column(p), f + p * V);
+    }
+    // Sums over the lanes of a row, of N values at once.  Rows of more than a wavefront go through LDS; `half` alternates between
+    // the two halves of it, so that one barrier a sum is enough.
+    template <int N> __device__ __forceinline__ void sum(float (&v)[N], float (*lds)[N_MAX][kWaves], int half) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = lanes_sum<(L < 64 ? L : 64)>(v[n]);
+        if constexpr (L > 64) {
+            const int wave = threadIdx.x >> 6, first = (int)threadIdx.x / L * (L / 64);
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) lds[half][n][wave] = v[n];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < L / 64; ++w) s += lds[half][n][first + w];
+                v[n] = s;
+            }
         }
-        const float2 st = row_stats(u, a.C, a.eps, lds);
-        T *y = static_cast<T *>(a.y) + row * a.ldy;
-        for (int c = threadIdx.x; c < a.C; c += kThreads)
-            from_f32(y[c], (to_f32(u[c]) - st.x) * st.y * (gamma ? to_f32(gamma[c]) : 1.f) + (beta ? to_f32(beta[c]) : 0.f));
     }
-}
+};
 
-template <typename T> __global__ __launch_bounds__(kThreads) void lnorm_stats_kernel(Args a)
+// u (zero where not owned) -> distances from the mean (zero where not owned), and the mean's and the variance's sums
+template <typename T, int L, int P, int V>
+__global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_fwd_kernel(Args a)
 {
-    __shared__ float lds[4];
-    for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float2 st = row_stats(static_cast<const T *>(a.x) + row * a.ldx, a.C, a.eps, lds);
-        if (threadIdx.x == 0) a.stats[row] = st;
-    }
-}
-
-template <typename T> __global__ __launch_bounds__(kThreads) void lnorm_bwd_kernel(Args a)
-{
-    __shared__ float lds[4];
-    const T *gamma = static_cast<const T *>(a.gamma);
-    for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *u = static_cast<const T *>(a.x) + row * a.ldx, *dy = static_cast<const T *>(a.dy) + row * a.ldy;
-        const float2 st = row_stats(u, a.C, a.eps, lds);
-        float sg = 0.f, sgx = 0.f;
-        for (int c = threadIdx.x; c < a.C; c += kThreads) {
-            const float g = to_f32(dy[c]) * (gamma ? to_f32(gamma[c]) : 1.f);
-            sg += g;
-            sgx += g * ((to_f32(u[c]) - st.x) * st.y);
+    using Pl = Place<L, P, V>;
+    __shared__ float lds[2][N_MAX][Pl::kWaves];
+    const Pl pl(a.C);
+    const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
+    const long stride = (long)gridDim.x * Pl::kGroups;
+    long row = (long)blockIdx.x * Pl::kGroups + (Pl::kGroups == 1 ? 0 : threadIdx.x / L);
+    Raw<T, V> gamma[P], beta[P], rx[P], rr[P];
+    pl.fetch_or(a.gamma, 1.f, gamma);
+    pl.fetch_or(a.beta, 0.f, beta);
+    // (a group of lanes past the last row goes along on that row and stores nothing)
+    const auto fetch = [&](long r) {
+        const long at = r < a.rows ? r : a.rows - 1;
+        pl.fetch(x + at * a.ldx, rx);
+        if (res) pl.fetch(res + at * a.ldr, rr);
+    };
+    const float per = 1.f / (float)a.C;
+    fetch(row);
+    for (long base = (long)blockIdx.x * Pl::kGroups; base < a.rows; base += stride, row += stride) {
+        float u[P * V];
+        const bool live = Pl::kGroups == 1 || row < a.rows;
+#pragma unroll
+        for (int p = 0; p < P; ++p) unpack(rx[p], u + p * V);
+        if (res) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float r[V];
+                unpack(rr[p], r);
+#pragma unroll
+                for (int i = 0; i < V; ++i) u[p * V + i] += r[i];
+                const Raw<T, V> held = pack(u + p * V, Raw<T, V>{}); // the norm is of what is stored
+                unpack(held, u + p * V);
+                if (live && pl.any(p)) __builtin_memcpy(static_cast<T *>(a.sum) + row * a.ldr + pl.column(p), &held.w, V * sizeof(T));
+            }
         }
-        sg = block_sum(sg, lds) / (float)a.C;
-        sgx = block_sum(sgx, lds) / (float)a.C;
-        T *dx = static_cast<T *>(a.dx) + row * a.ldr;
-        const T *ds = a.dsum ? static_cast<const T *>(a.dsum) + row * a.ldr : nullptr;
-        for (int c = threadIdx.x; c < a.C; c += kThreads) {
-            const float g = to_f32(dy[c]) * (gamma ? to_f32(gamma[c]) : 1.f);
-            from_f32(dx[c], (g - sg - (to_f32(u[c]) - st.x) * st.y * sgx) * st.y + (ds ? to_f32(ds[c]) : 0.f));
+        if (base + stride < a.rows) fetch(row + stride);
+        float s[1] = {0.f}, q[1] = {0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += pl.own(p, i) ? u[p * V + i] : 0.f;
+        pl.sum(s, lds, 0);
+        const float mean = s[0] / (float)a.C;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                u[p * V + i] -= mean;
+                q[0] += pl.own(p, i) ? u[p * V + i] * u[p * V + i] : 0.f;
+            }
+        pl.sum(q, lds, 1);
+        const float rstd = rsqrtf(q[0] * per + a.eps);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float f[V], e[V];
+            unpack(gamma[p], f);
+            unpack(beta[p], e);
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[p * V + i] = u[p * V + i] * rstd * f[i] + e[i];
         }
+        if (live) pl.put(static_cast<T *>(a.y) + row * a.ldy, u);
     }
 }
 
-// partial sums of dy * xh and dy over a slice of the rows, a thread per column
-template <typename T> __global__ __launch_bounds__(kThreads) void lnorm_wgrad_kernel(Args a)
+// dx of every row, and over the rows of a workgroup the sums of dy * xh and dy, a column in one place of one lane's registers throughout; they
+// leave as one vector of 2 C partial sums.
+template <typename T, int L, int P, int V, bool DSUM>
+__global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_bwd_kernel(Args a)
 {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= a.C) return;
-    float dg = 0.f, db = 0.f;
-    for (long row = blockIdx.y; row < a.rows; row += kSlices) {
-        const float2 st = a.stats[row];
-        const float d = to_f32(static_cast<const T *>(a.dy)[row * a.ldy + c]);
-        dg += d * ((to_f32(static_cast<const T *>(a.x)[row * a.ldx + c]) - st.x) * st.y);
-        db += d;
+    using Pl = Place<L, P, V>;
+    __shared__ float lds[2][N_MAX][Pl::kWaves];
+    const Pl pl(a.C);
+    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy), *ds = static_cast<const T *>(a.dsum);
+    const long stride = (long)gridDim.x * Pl::kGroups;
+    long row = (long)blockIdx.x * Pl::kGroups + (Pl::kGroups == 1 ? 0 : threadIdx.x / L);
+    Raw<T, V> gamma[P], rx[P], ry[P], rs[P];
+    pl.fetch_or(a.gamma, 1.f, gamma);
+    const auto fetch = [&](long r) {
+        const long at = r < a.rows ? r : a.rows - 1;
+        pl.fetch(x + at * a.ldx, rx);
+        pl.fetch(dy + at * a.ldy, ry);
+    };
+    float dg[P * V] = {}, db[P * V] = {};
+    const float per = 1.f / (float)a.C;
+    constexpr bool kAhead = L < 1024 && P * V <= 16; // (the next row's vectors beside this one's values: too much for the widest rows' registers)
+    if (kAhead) fetch(row);
+    for (long base = (long)blockIdx.x * Pl::kGroups; base < a.rows; base += stride, row += stride) {
+        float u[P * V], d[P * V];
+        const bool live = Pl::kGroups == 1 || row < a.rows;
+        if (!kAhead) fetch(row);
+        if constexpr (DSUM && kAhead) pl.fetch(ds + (live ? row : a.rows - 1) * a.ldr, rs);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            unpack(rx[p], u + p * V);
+            unpack(ry[p], d + p * V);
+        }
+        if (kAhead && base + stride < a.rows) fetch(row + stride);
+        if (!live) {
+#pragma unroll
+            for (int k = 0; k < P * V; ++k) d[k] = 0.f;
+        }
+        float s[1] = {0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += pl.own(p, i) ? u[p * V + i] : 0.f;
+        pl.sum(s, lds, 0);
+        const float mean = s[0] / (float)a.C;
+        // sums of the squared distances, of g and of g times the distance, in one round
+        float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float f[V];
+            unpack(gamma[p], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int k = p * V + i;
+                u[k] -= mean;
+                const float g = d[k] * f[i];
+                t[0] += pl.own(p, i) ? u[k] * u[k] : 0.f;
+                t[1] += pl.own(p, i) ? g : 0.f;
+                t[2] += pl.own(p, i) ? g * u[k] : 0.f;
+            }
+        }
+        pl.sum(t, lds, 1);
+        if constexpr (DSUM && !kAhead) pl.fetch(ds + (live ? row : a.rows - 1) * a.ldr, rs);
+        const float rstd = rsqrtf(t[0] * per + a.eps), sg = t[1] * per, sgx = t[2] * per * rstd;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float f[V], e[V];
+            again(gamma[p]);
+            unpack(gamma[p], f);
+            if constexpr (DSUM) unpack(rs[p], e);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int k = p * V + i;
+                const float xh = u[k] * rstd, g = d[k] * f[i];
+                dg[k] += d[k] * xh;
+                db[k] += d[k];
+                u[k] = (g - sg - xh * sgx) * rstd;
+                if constexpr (DSUM) u[k] += e[i];
+            }
+        }
+        if (live) pl.put(static_cast<T *>(a.dx) + row * a.ldr, u);
     }
-    float *part = a.part + (size_t)blockIdx.y * 2 * a.C;
-    part[c] = dg;
-    part[a.C + c] = db;
+    if (!a.part) return;
+    float *out = a.part + (size_t)blockIdx.x * 2 * a.C;
+    if constexpr (L < 256) {
+        // groups of a wavefront by exchanges between its lanes, then the wavefronts that hold the same columns one after the other in LDS
+        constexpr int kTurns = L <= 64 ? Pl::kWaves : Pl::kGroups;
+        __shared__ float acc[2][L * P * V];
+        const int turn = L <= 64 ? threadIdx.x >> 6 : threadIdx.x / L;
+#pragma unroll
+        for (int k = 0; k < P * V; ++k) {
+            if constexpr (L == 8) dg[k] = dpp_add<0x128>(dg[k]), db[k] = dpp_add<0x128>(db[k]); // (row_ror 8)
+            if constexpr (L <= 16) dg[k] = rows_add(dg[k]), db[k] = rows_add(db[k]);
+            if constexpr (L <= 32) dg[k] = halves_add(dg[k]), db[k] = halves_add(db[k]);
+        }
+        for (int w = 0; w < kTurns; ++w) {
+            if (turn == w && (L > 64 || (threadIdx.x & 63) < L)) {
+#pragma unroll
+                for (int k = 0; k < P * V; ++k) {
+                    const int at = k * L + pl.lane;
+                    acc[0][at] = w ? acc[0][at] + dg[k] : dg[k];
+                    acc[1][at] = w ? acc[1][at] + db[k] : db[k];
+                }
+            }
+            __syncthreads();
+        }
+        if (threadIdx.x < L) {
+#pragma unroll
+            for (int k = 0; k < P * V; ++k) dg[k] = acc[0][k * L + pl.lane], db[k] = acc[1][k * L + pl.lane];
+        }
+        if (threadIdx.x >= L) return;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (pl.any(p) && pl.own(p, i)) {
+                out[pl.column(p) + i] = dg[p * V + i];
+                out[a.C + pl.column(p) + i] = db[p * V + i];
+            }
 }
 
-__global__ __launch_bounds__(kThreads) void lnorm_sum_kernel(Args a)
+// The partial sums of kSumColumns columns: a slice of the workgroups per 32 threads, then the slices in their order.
+__global__ __launch_bounds__(kSumThreads) void lnorm_sum_kernel(Args a)
 {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= 2 * a.C) return;
+    constexpr int kSlices = kSumThreads / kSumColumns;
+    __shared__ float lds[kSlices][kSumColumns];
+    const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns, c = blockIdx.x * kSumColumns + col;
     float s = 0.f;
-    for (int i = 0; i < kSlices; ++i) s += a.part[(size_t)i * 2 * a.C + c];
+    if (c < 2 * a.C) {
+#pragma unroll 8
+        for (int i = slice; i < a.parts; i += kSlices) s += a.part[(size_t)i * 2 * a.C + c];
+    }
+    lds[slice][col] = s;
+    __syncthreads();
+    if (slice || c >= 2 * a.C) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i) s += lds[i][col];
     float *out = c < a.C ? a.dgamma + c : a.dbeta + (c - a.C);
     *out = a.accumulate ? *out + s : s;
 }
 
 struct Plan {
-    size_t elem, stats, part;
+    size_t elem, ws;
     long ldx, ldy, ldr;
+    int lanes, vectors; // L and P; lanes = 0: rows shorter than a vector
+    unsigned fwd_blocks, bwd_blocks;
 };
+
+// Lanes of a row: as few as hold it in 16 values each, but 512 with up to 32 for the widest fp32 rows (whose vectors, twice the size of bf16's, do not fit
+// the 128 registers that 16 wavefronts leave a lane).
+int lanes_of(int C, int V)
+{
+    int L = 8;
+    while (L * 16 < C && L < (V == 4 ? 512 : 1024)) L *= 2;
+    return L;
+}
 
 int make_plan(const lnorm_desc *d, Plan *p)
 {
@@ -140,18 +399,67 @@ int make_plan(const lnorm_desc *d, Plan *p)
     p->ldr = d->r_stride ? d->r_stride : d->C;
     if (p->ldx < d->C || p->ldy < d->C || p->ldr < d->C) return GSWA_EINVAL;
     p->elem = d->dtype == GSWA_F32 ? 4 : 2;
-    if (d->C > (int)(65536 / p->elem)) return GSWA_EUNSUPPORTED;
+    if (d->C > 16384) return GSWA_EUNSUPPORTED;
     const long widest = p->ldx > p->ldy ? (p->ldx > p->ldr ? p->ldx : p->ldr) : (p->ldy > p->ldr ? p->ldy : p->ldr);
     if (d->rows > (1L << 40) / widest) return GSWA_EUNSUPPORTED;
-    p->stats = to_256((size_t)d->rows * sizeof(float2));
-    p->part = to_256((size_t)kSlices * 2 * d->C * sizeof(float));
+    const int V = (int)(16 / p->elem), n = (d->C + V - 1) / V;
+    p->lanes = d->C < V ? 0 : lanes_of(d->C, V);
+    const int L = p->lanes ? p->lanes : 8, groups = L < 256 ? 256 / L : 1;
+    p->vectors = p->lanes ? (n + L - 1) / L : 1;
+    const long rows = (d->rows + groups - 1) / groups; // rounds of rows
+    const long cus = kSizingCus;
+    const long fwd = (L > 256 ? 2 : 8) * cus, bwd = (L > 256 ? 1 : L > 64 ? 2 : 4) * cus;
+    p->fwd_blocks = (unsigned)(rows < fwd ? rows : fwd);
+    p->bwd_blocks = (unsigned)(rows < bwd ? rows : bwd);
+    p->ws = to_256((size_t)p->bwd_blocks * 2 * d->C * sizeof(float));
     return GSWA_OK;
+}
+
+template <typename T, int L, int P, int V> void launch(const Args &a, const Plan &p, bool forward, hipStream_t st)
+{
+    const dim3 block(Place<L, P, V>::kBlock);
+    if (forward) hipLaunchKernelGGL((lnorm_fwd_kernel<T, L, P, V>), dim3(p.fwd_blocks), block, 0, st, a);
+    else if (a.dsum) hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, true>), dim3(p.bwd_blocks), block, 0, st, a);
+    else hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, false>), dim3(p.bwd_blocks), block, 0, st, a);
+}
+
+// (16 values are 2 vectors of bf16, 4 of fp32; rows of more than 128 values need more than half of that)
+template <typename T, int L> void launch_vectors(const Args &a, const Plan &p, bool forward, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (p.vectors == 16 / V) return launch<T, L, 16 / V, V>(a, p, forward, st);
+    if constexpr (V == 4) {
+        if (p.vectors == 3) return launch<T, L, 3, V>(a, p, forward, st);
+        if constexpr (L == 8)
+            if (p.vectors == 2) return launch<T, L, 2, V>(a, p, forward, st);
+        if constexpr (L == 512)
+            switch (p.vectors) {
+            case 5: return launch<T, L, 5, V>(a, p, forward, st);
+            case 6: return launch<T, L, 6, V>(a, p, forward, st);
+            case 7: return launch<T, L, 7, V>(a, p, forward, st);
+            case 8: return launch<T, L, 8, V>(a, p, forward, st);
+            }
+    }
+    if constexpr (L == 8) launch<T, L, 1, V>(a, p, forward, st);
+}
+
+template <typename T> void launch_type(const Args &a, const Plan &p, bool forward, hipStream_t st)
+{
+    switch (p.lanes) {
+    case 0: launch<T, 8, 1, 1>(a, p, forward, st); break;
+    case 8: launch_vectors<T, 8>(a, p, forward, st); break;
+    case 16: launch_vectors<T, 16>(a, p, forward, st); break;
+    case 32: launch_vectors<T, 32>(a, p, forward, st); break;
+    case 64: launch_vectors<T, 64>(a, p, forward, st); break;
+    case 128: launch_vectors<T, 128>(a, p, forward, st); break;
+    case 256: launch_vectors<T, 256>(a, p, forward, st); break;
+    case 512: launch_vectors<T, 512>(a, p, forward, st); break;
+    default: if constexpr (sizeof(T) == 2) launch_vectors<T, 1024>(a, p, forward, st);
+    }
 }
 
 // bytes from the first row's first value to the last row's last one
 size_t span(const lnorm_desc *d, const Plan &p, long ld) { return ((size_t)(d->rows - 1) * ld + d->C) * p.elem; }
-
-unsigned row_blocks(long rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
 
 } // namespace
 } // namespace gswa
@@ -171,7 +479,7 @@ int lnorm_query_bytes(const lnorm_desc *desc, size_t *bwd_ws_bytes)
     Plan p;
     const int rc = make_plan(desc, &p);
     if (rc != GSWA_OK) return rc;
-    if (bwd_ws_bytes) *bwd_ws_bytes = p.stats + p.part;
+    if (bwd_ws_bytes) *bwd_ws_bytes = p.ws;
     return GSWA_OK;
 }
 
@@ -193,8 +501,8 @@ int lnorm_forward(const lnorm_desc *desc, const void *x, const void *residual, c
     a.rows = desc->rows; a.ldx = p.ldx; a.ldy = p.ldy; a.ldr = p.ldr; a.C = desc->C; a.eps = desc->eps;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_LNORM_FWD, st);
-    if (desc->dtype == GSWA_F32) hipLaunchKernelGGL(lnorm_fwd_kernel<float>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(lnorm_fwd_kernel<bf16_t>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
+    if (desc->dtype == GSWA_F32) launch_type<float>(a, p, true, st);
+    else launch_type<bf16_t>(a, p, true, st);
     LN_LAUNCHED();
     return GSWA_OK;
 }
@@ -209,7 +517,7 @@ int lnorm_backward(const lnorm_desc *desc, const void *x, const void *dy, const 
     if (!aligned_to(16, x, dy, gamma, dsum, dx, dgamma, dbeta) || !aligned_to(256, ws)) return GSWA_EINVAL;
     const size_t row = (size_t)desc->C * p.elem, vec = (size_t)desc->C * sizeof(float);
     const Range rx(x, span(desc, p, p.ldx)), ry(dy, span(desc, p, p.ldy)), rg(gamma, row), rs(dsum, span(desc, p, p.ldr)),
-        rd(dx, span(desc, p, p.ldr)), wg(dgamma, vec), wb(dbeta, vec), rw(dgamma ? ws : nullptr, p.stats + p.part);
+        rd(dx, span(desc, p, p.ldr)), wg(dgamma, vec), wb(dbeta, vec), rw(dgamma ? ws : nullptr, p.ws);
     if (overlaps_any(rd, rx, rg, wg, wb, rw) || overlaps_any(wg, rx, ry, rg, rs, wb, rw) ||
         overlaps_any(wb, rx, ry, rg, rs, rw) || overlaps_any(rw, rx, ry, rg, rs))
         return GSWA_EINVAL;
@@ -219,29 +527,20 @@ int lnorm_backward(const lnorm_desc *desc, const void *x, const void *dy, const 
     a.x = x; a.dy = dy; a.gamma = gamma; a.dsum = dsum; a.dx = dx; a.dgamma = dgamma; a.dbeta = dbeta;
     a.rows = desc->rows; a.ldx = p.ldx; a.ldy = p.ldy; a.ldr = p.ldr; a.C = desc->C; a.eps = desc->eps;
     a.accumulate = (desc->flags & LNORM_ACCUM_WGRAD) != 0;
-    if (dgamma) {
-        a.stats = static_cast<float2 *>(ws);
-        a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + p.stats);
-    }
+    a.part = dgamma ? static_cast<float *>(ws) : nullptr;
+    a.parts = (int)p.bwd_blocks;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const bool f32 = desc->dtype == GSWA_F32;
-    // (dx may go over dy: the parameter gradients come first)
-    if (dgamma) {
-        const dim3 cols((desc->C + kThreads - 1) / kThreads, kSlices), both((2 * desc->C + kThreads - 1) / kThreads);
-        KernelTimer t(K_LNORM_SUM, st);
-        if (f32) hipLaunchKernelGGL(lnorm_stats_kernel<float>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(lnorm_stats_kernel<bf16_t>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
-        LN_LAUNCHED();
-        if (f32) hipLaunchKernelGGL(lnorm_wgrad_kernel<float>, cols, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(lnorm_wgrad_kernel<bf16_t>, cols, dim3(kThreads), 0, st, a);
-        LN_LAUNCHED();
-        hipLaunchKernelGGL(lnorm_sum_kernel, both, dim3(kThreads), 0, st, a);
+    {
+        KernelTimer t(K_LNORM_BWD, st);
+        if (desc->dtype == GSWA_F32) launch_type<float>(a, p, false, st);
+        else launch_type<bf16_t>(a, p, false, st);
         LN_LAUNCHED();
     }
-    KernelTimer t(K_LNORM_BWD, st);
-    if (f32) hipLaunchKernelGGL(lnorm_bwd_kernel<float>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(lnorm_bwd_kernel<bf16_t>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, st, a);
-    LN_LAUNCHED();
+    if (dgamma) {
+        KernelTimer t(K_LNORM_SUM, st);
+        hipLaunchKernelGGL(lnorm_sum_kernel, dim3((2 * desc->C + kSumColumns - 1) / kSumColumns), dim3(kSumThreads), 0, st, a);
+        LN_LAUNCHED();
+    }
     return GSWA_OK;
 }
 

@@ -35,7 +35,7 @@ def test_exports():
     (dict(rows=0), gswa.GSWA_EINVAL), (dict(rows=-1), gswa.GSWA_EINVAL), (dict(C=0), gswa.GSWA_EINVAL), (dict(dtype=2), gswa.GSWA_EINVAL),
     (dict(eps=-1.0), gswa.GSWA_EINVAL), (dict(eps=float("nan")), gswa.GSWA_EINVAL), (dict(flags=2), gswa.GSWA_EINVAL),
     (dict(x_stride=59), gswa.GSWA_EINVAL), (dict(y_stride=-60), gswa.GSWA_EINVAL), (dict(r_stride=1), gswa.GSWA_EINVAL),
-    (dict(C=32769), gswa.GSWA_EUNSUPPORTED), (dict(C=16385, dtype="f32"), gswa.GSWA_EUNSUPPORTED),
+    (dict(C=16385), gswa.GSWA_EUNSUPPORTED), (dict(C=16385, dtype="f32"), gswa.GSWA_EUNSUPPORTED),
     (dict(rows=1 << 40, C=60), gswa.GSWA_EUNSUPPORTED),
 ])
 def test_bad_descriptors(change, status):
@@ -45,7 +45,7 @@ def test_bad_descriptors(change, status):
 
 
 def test_scratch_is_a_multiple_of_256():
-    for rows, C in ((1, 1), (7, 60), (131072, 180), (4096, 32768)):
+    for rows, C in ((1, 1), (7, 60), (131072, 180), (4096, 16384)):
         n = lnorm.lnorm_query_bytes(lnorm.make_desc(rows, C, "bf16"))
         assert n > 0 and n % 256 == 0
 
@@ -164,15 +164,13 @@ def _check(rows, C, dtype, residual=False, affine=True, xs=0, ys=0, rs=0, eps=1e
 
 # every width of the row variants and next to their borders; odd ones; C below a vector
 WIDTHS = [1, 2, 3, 7, 8, 9, 31, 60, 64, 65, 127, 128, 129, 180, 192, 255, 256, 257, 360, 511, 512, 513, 1000, 1024, 1025, 1536, 2047, 2048, 2049, 4096,
-          4100, 8191, 8192, 8193, 16384]
+          4100, 8191, 8192, 8193, 12289, 16383, 16384]
 
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("C", WIDTHS + [20001, 32768])
+@pytest.mark.parametrize("C", WIDTHS)
 def test_widths(C, dtype):
-    if C > 16384 and dtype == "f32":
-        pytest.skip("refused")
     _check(37 if C < 4096 else 5, C, dtype, residual=C % 2 == 0, seed=C)
 
 
