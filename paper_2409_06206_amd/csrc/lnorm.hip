@@ -111,8 +111,8 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v)
 // The L lanes of a row, and what each holds of it: vector p of a lane is columns [column(p), column(p) + V).  The row's last vector ends
 // at column C: where C is no multiple of V it begins inside the one before it, whose columns it reads as well but does not own.  (So no load or store
 // is ever narrower than a vector; both lanes store the same values.)
-template <int L, int P, int V> struct Place {
-    static constexpr int kBlock = L > 256 ? L : 256, kGroups = kBlock / L, kWaves = kBlock / 64;
+template <int L, int P, int V, int THREADS> struct Place {
+    static constexpr int kBlock = THREADS, kGroups = kBlock / L, kWaves = kBlock / 64;
     int C, lane;
     __device__ __forceinline__ Place(int C_) : C(C_), lane((int)threadIdx.x % L) {}
     __device__ __forceinline__ int column(int p) const
@@ -164,11 +164,15 @@ template <int L, int P, int V> struct Place {
     }
 };
 
-// u (zero where not owned) -> distances from the mean (zero where not owned), and the mean's and the variance's sums
+// Threads of a workgroup.  The backward pass leaves one vector of partial sums per workgroup, so where no barrier ties its rows together it has half as many,
+// of twice the size, if the registers allow four wavefronts on a SIMD anyway.
+template <int L> constexpr int fwd_threads() { return L > 256 ? L : 256; }
+constexpr int bwd_threads(int L, int values, int V) { return L > 256 || (L <= 64 && values <= (V == 4 ? 8 : 16)) ? 512 : 256; }
+
 template <typename T, int L, int P, int V>
-__global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_fwd_kernel(Args a)
+__global__ __launch_bounds__((fwd_threads<L>())) void lnorm_fwd_kernel(Args a)
 {
-    using Pl = Place<L, P, V>;
+    using Pl = Place<L, P, V, fwd_threads<L>()>;
     __shared__ float lds[2][N_MAX][Pl::kWaves];
     const Pl pl(a.C);
     const T *x = static_cast<const T *>(a.x), *res = static_cast<const T *>(a.residual);
@@ -234,9 +238,9 @@ __global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_fwd_kernel(Arg
 // dx of every row, and over the rows of a workgroup the sums of dy * xh and dy, a column in one place of one lane's registers throughout; they
 // leave as one vector of 2 C partial sums.
 template <typename T, int L, int P, int V, bool DSUM>
-__global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_bwd_kernel(Args a)
+__global__ __launch_bounds__((bwd_threads(L, P * V, V))) void lnorm_bwd_kernel(Args a)
 {
-    using Pl = Place<L, P, V>;
+    using Pl = Place<L, P, V, bwd_threads(L, P * V, V)>;
     __shared__ float lds[2][N_MAX][Pl::kWaves];
     const Pl pl(a.C);
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy), *ds = static_cast<const T *>(a.dsum);
@@ -251,7 +255,7 @@ __global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_bwd_kernel(Arg
     };
     float dg[P * V] = {}, db[P * V] = {};
     const float per = 1.f / (float)a.C;
-    constexpr bool kAhead = L < 1024 && P * V <= 16; // (the next row's vectors beside this one's values: too much for the widest rows' registers)
+    constexpr bool kAhead = P * V <= (V == 8 ? 24 : 16); // (the next row's vectors beside this one's values: too much for the widest rows' registers)
     if (kAhead) fetch(row);
     for (long base = (long)blockIdx.x * Pl::kGroups; base < a.rows; base += stride, row += stride) {
         float u[P * V], d[P * V];
@@ -314,7 +318,7 @@ __global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_bwd_kernel(Arg
     }
     if (!a.part) return;
     float *out = a.part + (size_t)blockIdx.x * 2 * a.C;
-    if constexpr (L < 256) {
+    if constexpr (Pl::kGroups > 1) {
         // groups of a wavefront by exchanges between its lanes, then the wavefronts that hold the same columns one after the other in LDS
         constexpr int kTurns = L <= 64 ? Pl::kWaves : Pl::kGroups;
         __shared__ float acc[2][L * P * V];
@@ -343,13 +347,19 @@ __global__ __launch_bounds__((Place<L, P, V>::kBlock)) void lnorm_bwd_kernel(Arg
         if (threadIdx.x >= L) return;
     }
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+        if (pl.any(p) && pl.own(p, 0)) { // a whole vector of its own
+            __builtin_memcpy(out + pl.column(p), dg + p * V, V * sizeof(float));
+            __builtin_memcpy(out + a.C + pl.column(p), db + p * V, V * sizeof(float));
+        } else if (pl.any(p)) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (pl.any(p) && pl.own(p, i)) {
-                out[pl.column(p) + i] = dg[p * V + i];
-                out[a.C + pl.column(p) + i] = db[p * V + i];
-            }
+            for (int i = 1; i < V; ++i)
+                if (pl.own(p, i)) {
+                    out[pl.column(p) + i] = dg[p * V + i];
+                    out[a.C + pl.column(p) + i] = db[p * V + i];
+                }
+        }
+    }
 }
 
 // The partial sums of kSumColumns columns: a slice of the workgroups per 32 threads, then the slices in their order.
@@ -380,12 +390,14 @@ struct Plan {
     unsigned fwd_blocks, bwd_blocks;
 };
 
-// Lanes of a row: as few as hold it in 16 values each, but 512 with up to 32 for the widest fp32 rows (whose vectors, twice the size of bf16's, do not fit
-// the 128 registers that 16 wavefronts leave a lane).
+// Lanes of a row: as few as hold it in 24 values of bf16 or 16 of fp32 each, at most 512, which hold the widest rows in 32.  (Fewer lanes with more
+// values keep more loads in flight and leave fewer lanes idle behind the row's end; the backward pass has two fp32 sums for each value in registers as
+// well.  Backward of 8192 x 5120 bf16 without parameter gradients: 640 vectors on 256 lanes 48.2 us, on 512 58.1 us; 4096 x 12288: on 512
+// 57.5 us, on 1024 74.2 us.)
 int lanes_of(int C, int V)
 {
     int L = 8;
-    while (L * 16 < C && L < (V == 4 ? 512 : 1024)) L *= 2;
+    while (L * (V == 8 ? 24 : 16) < C && L < 512) L *= 2;
     return L;
 }
 
@@ -404,43 +416,42 @@ int make_plan(const lnorm_desc *d, Plan *p)
     if (d->rows > (1L << 40) / widest) return GSWA_EUNSUPPORTED;
     const int V = (int)(16 / p->elem), n = (d->C + V - 1) / V;
     p->lanes = d->C < V ? 0 : lanes_of(d->C, V);
-    const int L = p->lanes ? p->lanes : 8, groups = L < 256 ? 256 / L : 1;
+    const int L = p->lanes ? p->lanes : 8;
     p->vectors = p->lanes ? (n + L - 1) / L : 1;
-    const long rows = (d->rows + groups - 1) / groups; // rounds of rows
-    const long cus = kSizingCus;
-    const long fwd = (L > 256 ? 2 : 8) * cus, bwd = (L > 256 ? 1 : L > 64 ? 2 : 4) * cus;
-    p->fwd_blocks = (unsigned)(rows < fwd ? rows : fwd);
-    p->bwd_blocks = (unsigned)(rows < bwd ? rows : bwd);
+    const int values = p->vectors * (p->lanes ? V : 1);
+    // workgroups: what the compute units hold at once, going on to further rows
+    const auto blocks = [&](int threads, long most) {
+        const long rounds = (d->rows + threads / L - 1) / (threads / L);
+        return (unsigned)(rounds < most ? rounds : most);
+    };
+    p->fwd_blocks = blocks(L > 256 ? L : 256, (L > 256 ? 4 : 8) * kSizingCus);
+    p->bwd_blocks = blocks(bwd_threads(L, values, p->lanes ? V : 1), (L > 256 && values > 16 ? 1 : L <= 64 && V == 4 && values > 8 ? 3 : 2) * kSizingCus);
     p->ws = to_256((size_t)p->bwd_blocks * 2 * d->C * sizeof(float));
     return GSWA_OK;
 }
 
 template <typename T, int L, int P, int V> void launch(const Args &a, const Plan &p, bool forward, hipStream_t st)
 {
-    const dim3 block(Place<L, P, V>::kBlock);
-    if (forward) hipLaunchKernelGGL((lnorm_fwd_kernel<T, L, P, V>), dim3(p.fwd_blocks), block, 0, st, a);
-    else if (a.dsum) hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, true>), dim3(p.bwd_blocks), block, 0, st, a);
-    else hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, false>), dim3(p.bwd_blocks), block, 0, st, a);
+    const dim3 fwd(fwd_threads<L>()), bwd(bwd_threads(L, P * V, V));
+    if (forward) hipLaunchKernelGGL((lnorm_fwd_kernel<T, L, P, V>), dim3(p.fwd_blocks), fwd, 0, st, a);
+    else if (a.dsum) hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, true>), dim3(p.bwd_blocks), bwd, 0, st, a);
+    else hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, false>), dim3(p.bwd_blocks), bwd, 0, st, a);
 }
 
-// (16 values are 2 vectors of bf16, 4 of fp32; rows of more than 128 values need more than half of that)
+// The numbers of vectors that lanes_of leads to: more than half of the most, but on 8 lanes, and up to 32 values on 512.
 template <typename T, int L> void launch_vectors(const Args &a, const Plan &p, bool forward, hipStream_t st)
 {
     constexpr int V = 16 / sizeof(T);
-    if (p.vectors == 16 / V) return launch<T, L, 16 / V, V>(a, p, forward, st);
-    if constexpr (V == 4) {
-        if (p.vectors == 3) return launch<T, L, 3, V>(a, p, forward, st);
-        if constexpr (L == 8)
-            if (p.vectors == 2) return launch<T, L, 2, V>(a, p, forward, st);
-        if constexpr (L == 512)
-            switch (p.vectors) {
-            case 5: return launch<T, L, 5, V>(a, p, forward, st);
-            case 6: return launch<T, L, 6, V>(a, p, forward, st);
-            case 7: return launch<T, L, 7, V>(a, p, forward, st);
-            case 8: return launch<T, L, 8, V>(a, p, forward, st);
-            }
+    switch (p.vectors) {
+    case 1: if constexpr (L == 8) launch<T, L, 1, V>(a, p, forward, st); break;
+    case 2: if constexpr (L == 8 || V == 8) launch<T, L, 2, V>(a, p, forward, st); break;
+    case 3: launch<T, L, 3, V>(a, p, forward, st); break;
+    case 4: if constexpr (L == 512 || V == 4) launch<T, L, 4, V>(a, p, forward, st); break;
+    case 5: if constexpr (L == 512 && V == 4) launch<T, L, 5, V>(a, p, forward, st); break;
+    case 6: if constexpr (L == 512 && V == 4) launch<T, L, 6, V>(a, p, forward, st); break;
+    case 7: if constexpr (L == 512 && V == 4) launch<T, L, 7, V>(a, p, forward, st); break;
+    case 8: if constexpr (L == 512 && V == 4) launch<T, L, 8, V>(a, p, forward, st); break;
     }
-    if constexpr (L == 8) launch<T, L, 1, V>(a, p, forward, st);
 }
 
 template <typename T> void launch_type(const Args &a, const Plan &p, bool forward, hipStream_t st)
@@ -454,7 +465,6 @@ template <typename T> void launch_type(const Args &a, const Plan &p, bool forwar
     case 128: launch_vectors<T, 128>(a, p, forward, st); break;
     case 256: launch_vectors<T, 256>(a, p, forward, st); break;
     case 512: launch_vectors<T, 512>(a, p, forward, st); break;
-    default: if constexpr (sizeof(T) == 2) launch_vectors<T, 1024>(a, p, forward, st);
     }
 }
 
