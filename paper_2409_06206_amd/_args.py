@@ -3,32 +3,45 @@
 A tensor of the wrong type, size or layout would be read out of its bounds by a kernel; raw addresses (integers) are the
 caller's own.  Work goes to the device the tensors lie on and, where no stream is named, to that device's current stream.
 """
-from .gswa import GSWA_BF16, GSWA_F32, _check
+import torch
+
+from .gswa import GSWA_BF16, GSWA_F32, GSWA_OK, _check
 
 DTYPES = {"f32": GSWA_F32, "bf16": GSWA_BF16}
+TORCH_DTYPES = {GSWA_F32: torch.float32, GSWA_BF16: torch.bfloat16}
+# (the handle alone: torch.cuda.current_stream() builds a stream object around it, 1.8 us of a call of 5)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def torch_dtype(code):
+    return TORCH_DTYPES.get(code, torch.bfloat16)   # (a code that is none is refused by the library)
 
 
 class Call:
-    """One call: collects the device of its tensors."""
+    """One call: `device` is the index of the device its tensors lie on, None before the first."""
 
-    def __init__(self):
-        self.device = None
+    __slots__ = ("device",)
 
-    def _seen(self, name, t, dtype):
-        if not t.is_cuda:
+    def __init__(self, device=None):
+        self.device = device
+
+    def _place(self, name, t, dtype):
+        at = t.get_device()
+        if at < 0:
             raise ValueError(f"{name} must lie on a GPU")
         if self.device is None:
-            self.device = t.device
-        elif t.device != self.device:
-            raise ValueError(f"{name} lies on {t.device}, the tensors before it on {self.device}")
-        if dtype is not None and t.dtype != dtype:
+            self.device = at
+        elif at != self.device:
+            raise ValueError(f"{name} lies on device {at}, the tensors before it on device {self.device}")
+        if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
 
     def flat(self, name, t, dtype, numel):
         """Address of a contiguous tensor of at least `numel` elements."""
-        if t is None or isinstance(t, int):
+        if t is None or t.__class__ is int:
             return t
-        self._seen(name, t, dtype)
+        if t.get_device() != self.device or t.dtype is not dtype:
+            self._place(name, t, dtype)
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.numel() < numel:
@@ -37,14 +50,16 @@ class Call:
 
     def rows(self, name, t, dtype, rows, length, stride):
         """Address of `rows` rows of `length` elements, `stride` apart: contiguous in any shape, or 2-D."""
-        if t is None or isinstance(t, int):
+        if t is None or t.__class__ is int:
             return t
-        self._seen(name, t, dtype)
+        if t.get_device() != self.device or t.dtype is not dtype:
+            self._place(name, t, dtype)
+        if t.shape == (rows, length) and t.stride() == (stride, 1):
+            return t.data_ptr()
         if t.is_contiguous() and (stride == length or rows == 1):
             if t.numel() != rows * length or t.shape[-1] != length:
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, {rows} rows of {length} are needed")
-        elif t.dim() != 2 or tuple(t.shape) != (rows, length) or (length > 1 and t.stride(1) != 1) or \
-                (rows > 1 and t.stride(0) != stride):
+        elif t.dim() != 2 or t.shape != (rows, length) or (length > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != stride):
             raise ValueError(f"{name} must be {rows} rows of {length} elements, {stride} apart; it has shape {tuple(t.shape)} "
                              f"and strides {t.stride()}")
         return t.data_ptr()
@@ -53,24 +68,19 @@ class Call:
         """fn(*args, stream) on the tensors' device."""
         if self.device is None:       # raw addresses only
             if stream is None:
-                import torch
                 stream = torch.cuda.current_stream()
             _check(fn(*args, getattr(stream, "cuda_stream", stream)))
             return
-        import torch
-        at = getattr(stream, "device", None)
-        if at is not None and at != self.device:
-            raise ValueError(f"the stream belongs to {at}, the tensors lie on {self.device}")
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        handle = getattr(stream, "cuda_stream", stream)
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(*args, handle))
+            stream = _raw_stream(self.device)
+        elif not isinstance(stream, int):
+            if stream.device_index != self.device:
+                raise ValueError(f"the stream belongs to device {stream.device_index}, the tensors lie on device {self.device}")
+            stream = stream.cuda_stream
+        if torch.cuda.current_device() == self.device:
+            status = fn(*args, stream)
+            if status != GSWA_OK:
+                _check(status)
         else:
             with torch.cuda.device(self.device):
-                _check(fn(*args, handle))
-
-
-def torch_dtype(code):
-    import torch
-    return torch.float32 if code == GSWA_F32 else torch.bfloat16
+                _check(fn(*args, stream))

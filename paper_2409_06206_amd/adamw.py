@@ -5,6 +5,8 @@ is an error, there is no fallback path.
 """
 import ctypes
 
+import torch
+
 from . import gswa
 from ._args import Call
 from .gswa import GSWA_BF16, GSWA_F32, _check
@@ -52,40 +54,43 @@ def make_desc(beta1=0.9, beta2=0.999, eps=1e-8, state_bits=32, flags=0, seed=0):
     return adamw_desc(beta1, beta2, eps, state_bits, flags, seed)
 
 
-def _dtype(name, t):
-    import torch
-    code = {torch.float32: GSWA_F32, torch.bfloat16: GSWA_BF16}.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
-    return code
+_FIELDS = frozenset(("p", "master", "g", "m", "v", "m_exp", "v_exp", "weight_decay"))
+_CODES = {torch.float32: GSWA_F32, torch.bfloat16: GSWA_BF16}
 
 
-def _list(desc, tensors, c):
-    import torch
-    state = torch.uint8 if desc.state_bits == 8 else torch.float32
+def _list(desc, tensors):
+    """The C list of tensors and the index of the device they lie on."""
+    c, eight = Call(), desc.state_bits == 8
+    state = torch.uint8 if eight else torch.float32
     out = (adamw_tensor * len(tensors))()
     for i, part in enumerate(tensors):
-        unknown = set(part) - {"p", "master", "g", "m", "v", "m_exp", "v_exp", "weight_decay"}
-        if unknown:
-            raise ValueError(f"tensor {i}: unknown fields {sorted(unknown)}")
-        p, g, n = part["p"], part["g"], part["p"].numel()
+        if not _FIELDS.issuperset(part):
+            raise ValueError(f"tensor {i}: unknown fields {sorted(set(part) - _FIELDS)}")
+        p, g, master = part["p"], part["g"], part.get("master")
+        n, row = p.numel(), out[i]
         if g.numel() != n:
             raise ValueError(f"tensor {i}: {n} parameters, {g.numel()} gradients")
-        need = {"p": (p.dtype, n), "g": (g.dtype, n), "m": (state, n), "v": (state, n)}
-        if part.get("master") is not None:
-            need["master"] = (torch.float32, n)
-        if desc.state_bits == 8:
-            need.update({k: (torch.uint8, -(-n // BLOCK)) for k in ("m_exp", "v_exp")})
-        places = {k: c.flat(f"{k} of tensor {i}", part[k], *need[k]) for k in need}
-        out[i] = adamw_tensor(n, _dtype("p", p), _dtype("g", g), part.get("weight_decay", 0.0), **places)
-    return out
+        if p.dtype not in _CODES or g.dtype not in _CODES:
+            raise ValueError(f"tensor {i}: parameters and gradients must be float32 or bfloat16, not {p.dtype} and {g.dtype}")
+        try:
+            row.n, row.p_dtype, row.g_dtype, row.weight_decay = n, _CODES[p.dtype], _CODES[g.dtype], part.get("weight_decay", 0.0)
+            row.p, row.g = c.flat("p", p, p.dtype, n), c.flat("g", g, g.dtype, n)
+            row.m, row.v = c.flat("m", part["m"], state, n), c.flat("v", part["v"], state, n)
+            if master is not None:
+                row.master = c.flat("master", master, torch.float32, n)
+            if eight:
+                blocks = -(-n // BLOCK)
+                row.m_exp, row.v_exp = c.flat("m_exp", part["m_exp"], torch.uint8, blocks), c.flat("v_exp", part["v_exp"], torch.uint8, blocks)
+        except ValueError as e:
+            raise ValueError(f"tensor {i}: {e}") from None
+    return out, c.device
 
 
 class Plan:
     """A plan with what keeps its memory alive."""
 
     def __init__(self, tensors, buffer):
-        self.c_plan, self.tensors, self.buffer = adamw_plan_t(), tensors, buffer
+        self.c_plan, self.tensors, self.buffer, self.device = adamw_plan_t(), tensors, buffer, buffer.get_device()
 
     @property
     def elements(self):
@@ -95,17 +100,18 @@ class Plan:
 
 def adamw_query_bytes(desc, tensors):
     """Bytes of a plan's buffer.  tensors: list of dicts with p, g, m, v and, where they apply, master, m_exp, v_exp, weight_decay."""
-    n = ctypes.c_size_t()
-    _check(lib().adamw_query_bytes(ctypes.byref(desc), _list(desc, tensors, Call()), len(tensors), ctypes.byref(n)))
+    n, sizes = ctypes.c_size_t(), (adamw_tensor * len(tensors))()
+    for row, part in zip(sizes, tensors):
+        row.n = part["p"].numel()
+    _check(lib().adamw_query_bytes(ctypes.byref(desc), sizes, len(tensors), ctypes.byref(n)))
     return n.value
 
 
 def adamw_plan(desc, tensors, buffer, stream=None):
     """The Plan that the calls below take; it keeps the tensors and the buffer alive."""
-    import torch
-    L, c = lib(), Call()
-    listed = _list(desc, tensors, c)
-    n = ctypes.c_size_t()
+    L, n = lib(), ctypes.c_size_t()
+    listed, device = _list(desc, tensors)
+    c = Call(device)
     _check(L.adamw_query_bytes(ctypes.byref(desc), listed, len(tensors), ctypes.byref(n)))
     plan = Plan([dict(t) for t in tensors], buffer)
     c.run(L.adamw_plan, stream, ctypes.byref(desc), listed, len(tensors), c.flat("buffer", buffer, torch.uint8, n.value),
@@ -113,27 +119,18 @@ def adamw_plan(desc, tensors, buffer, stream=None):
     return plan
 
 
-def _call(plan):
-    c = Call()
-    c.device = plan.buffer.device
-    return c
-
-
 def adamw_norm(plan, norm, stream=None):
-    import torch
-    c = _call(plan)
+    c = Call(plan.device)
     c.run(lib().adamw_norm, stream, ctypes.byref(plan.c_plan), c.flat("norm", norm, torch.float32, 1))
 
 
 def adamw_step(plan, step, lr, lr_scale=None, norm=None, max_norm=0.0, stream=None):
-    import torch
-    c = _call(plan)
+    c = Call(plan.device)
     c.run(lib().adamw_step, stream, ctypes.byref(plan.c_plan), c.flat("step", step, torch.int64, 1), lr,
           c.flat("lr_scale", lr_scale, torch.float32, 1), c.flat("norm", norm, torch.float32, 1), max_norm)
 
 
 def adamw_unpack(plan, m_out, v_out, stream=None):
-    import torch
-    c = _call(plan)
+    c = Call(plan.device)
     c.run(lib().adamw_unpack, stream, ctypes.byref(plan.c_plan), c.flat("m_out", m_out, torch.bfloat16, plan.elements),
           c.flat("v_out", v_out, torch.bfloat16, plan.elements))

@@ -2,6 +2,7 @@
 #include "../../include/relpos.h"
 #include "args.h"
 #include "common.h"
+#include "mfma.h"
 #include "profile.h"
 
 #include <math.h>
@@ -11,131 +12,350 @@ namespace gswa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 64; // rows of a gradient (one image and head) that one workgroup sums
+constexpr int kRows = 64;         // rows of a tile of the gradient, one lane of the values that leave it each
+constexpr int kMostFwdRows = 64;  // rows of a tile of the bias, at most
 
 struct Args {
     const void *table, *dout;
     void *out;
     float *dtable, *part; // part: [heads][slices][buckets]
-    long ld, slices;
+    long ld;
     int heads, batch, q, k, start, window, buckets, bidirectional, causal, accumulate, n;
+    int rows, slices;     // rows of a tile of the bias; workgroups of a head in the sums of the gradient
     int edges[RELPOS_MAX_EDGES];
 };
 
 // edges <= d
-__device__ __forceinline__ int edges_up_to(const Args &a, int d)
+template <typename E> __device__ __forceinline__ int edges_up_to(const E *edges, int n, int d)
 {
-    int lo = 0, hi = a.n;
+    int lo = 0, hi = n;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (a.edges[mid] <= d) lo = mid + 1;
+        if (edges[mid] <= d) lo = mid + 1;
         else hi = mid;
     }
     return lo;
 }
 
-// bucket of r = key - query
-__device__ __forceinline__ int bucket_of(const Args &a, int r)
-{
-    if (!a.bidirectional) return edges_up_to(a, r < 0 ? -r : 0);
-    return edges_up_to(a, r < 0 ? -r : r) + (r > 0 ? a.n + 1 : 0);
-}
-
-__device__ __forceinline__ int window_bucket(const Args &a, int offset)
-{
-    const int side = 2 * a.window - 1;
-    const int dr = offset / side - (a.window - 1), dc = offset % side - (a.window - 1);
-    return bucket_of(a, -dr) * 2 * (a.n + 1) + bucket_of(a, -dc);
-}
+// ---- the table of a window --------------------------------------------------------------------------------------------------------
+// A few thousand values: what counts is the chain of dependent steps.  The buckets of the 2 M - 1 offsets of an axis are found side by side and kept
+// in LDS; a pair of buckets is a rectangle of offsets, which one wavefront sums.
 
 template <typename T> __global__ __launch_bounds__(kThreads) void window_fwd_kernel(Args a)
 {
-    const int side = 2 * a.window - 1, total = side * side * a.heads;
+    __shared__ int axis[128];
+    const int side = 2 * a.window - 1, total = side * side * a.heads, B = 2 * (a.n + 1);
+    if ((int)threadIdx.x < side) {
+        const int r = a.window - 1 - (int)threadIdx.x, d = r < 0 ? -r : r; // key - query of the offset query - key = threadIdx.x - (M - 1)
+        int n = 0;
+        for (int e = 0; e < a.n; ++e) n += a.edges[e] <= d;
+        axis[threadIdx.x] = n + (r > 0 ? a.n + 1 : 0);
+    }
+    __syncthreads();
     const int e = blockIdx.x * kThreads + threadIdx.x;
     if (e >= total) return;
-    const int offset = e / a.heads, h = e - offset * a.heads;
-    static_cast<T *>(a.out)[e] = static_cast<const T *>(a.table)[(long)window_bucket(a, offset) * a.heads + h];
+    const int offset = e / a.heads, h = e - offset * a.heads, dr = offset / side, dc = offset - dr * side;
+    static_cast<T *>(a.out)[e] = static_cast<const T *>(a.table)[((long)axis[dr] * B + axis[dc]) * a.heads + h];
 }
 
-// a thread per learned value goes over the offsets of its pair of buckets
+// The places [lo, hi) of an axis of the table whose offsets fall into bucket b.
+__device__ __forceinline__ void bucket_places(const Args &a, int b, int &lo, int &hi)
+{
+    const int M = a.window, behind = b > a.n, n = behind ? b - a.n - 1 : b;
+    const int from = n ? a.edges[n - 1] : behind, to = n < a.n ? a.edges[n] - 1 : M - 1; // distances; key behind the query: r > 0
+    const int first = from, last = to < M - 1 ? to : M - 1;
+    // place = query - key + M - 1 = M - 1 - r
+    lo = behind ? M - 1 - last : M - 1 + first;
+    hi = behind ? M - first : M + last;
+    if (first > last) lo = hi = 0;
+}
+
+// A wavefront per pair of buckets: its lanes take the heads of as many places at once as there is room for, places in their order; the lanes of a
+// head are summed in their order.
 __global__ __launch_bounds__(kThreads) void window_bwd_kernel(Args a)
 {
-    const int side = 2 * a.window - 1;
-    const int e = blockIdx.x * kThreads + threadIdx.x;
-    if (e >= a.buckets * a.heads) return;
-    const int b = e / a.heads, h = e - b * a.heads;
-    float s = 0.f;
-    for (int o = 0; o < side * side; ++o)
-        if (window_bucket(a, o) == b) s += static_cast<const float *>(a.dout)[(long)o * a.heads + h];
-    a.dtable[e] = a.accumulate ? a.dtable[e] + s : s;
-}
-
-template <typename T> __global__ __launch_bounds__(kThreads) void sequence_fwd_kernel(Args a)
-{
-    const int h = blockIdx.y;
-    for (int i = blockIdx.x; i < a.q; i += gridDim.x) {
-        T *row = static_cast<T *>(a.out) + ((long)h * a.q + i) * a.ld;
-        for (int j = threadIdx.x; j < a.k; j += kThreads) {
-            const int r = j - i - a.start;
-            if (a.causal && r > 0) from_f32(row[j], -INFINITY);
-            else row[j] = static_cast<const T *>(a.table)[(long)bucket_of(a, r) * a.heads + h];
-        }
+    __shared__ float lds[kThreads];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, B = 2 * (a.n + 1), side = 2 * a.window - 1;
+    const int pair = blockIdx.x * (kThreads / 64) + wave;
+    int r0 = 0, r1 = 0, c0 = 0, c1 = 0;
+    if (pair < B * B) {
+        bucket_places(a, pair / B, r0, r1);
+        bucket_places(a, pair % B, c0, c1);
     }
-}
-
-// A workgroup sums kRows rows of one image and head.  A thread walks down a diagonal (key - query = const, one bucket), neighbours next to
-// each other in every row; 256 diagonals at a time go to LDS, where a thread per bucket adds those of its bucket in their order.
-template <typename T> __global__ __launch_bounds__(kThreads) void sequence_bwd_kernel(Args a)
-{
-    __shared__ float sums[kThreads];
-    __shared__ int of[kThreads];
-    const int h = blockIdx.y;
-    const int slices_q = (a.q + kRows - 1) / kRows;
-    for (long slice = blockIdx.x; slice < a.slices; slice += gridDim.x) {
-        const int b = (int)(slice / slices_q), i0 = (int)(slice % slices_q) * kRows, i1 = i0 + kRows < a.q ? i0 + kRows : a.q;
-        const T *d = static_cast<const T *>(a.dout) + ((long)b * a.heads + h) * a.q * a.ld;
-        // the diagonals that meet these rows: from the last row's first key to the first row's last one (or to the query itself)
-        const int first = -(i1 - 1), last = a.causal && a.start < a.k - 1 - i0 ? a.start : a.k - 1 - i0; // j - i
-        float mine = 0.f;
-        for (int c0 = first; c0 <= last; c0 += kThreads) {
-            const int diag = c0 + (int)threadIdx.x;
-            float s = 0.f;
-            if (diag <= last)
-                for (int i = i0; i < i1; ++i) {
-                    const int j = i + diag;
-                    if (j >= 0 && j < a.k) s += to_f32(d[(long)i * a.ld + j]);
-                }
-            __syncthreads();
-            sums[threadIdx.x] = s;
-            of[threadIdx.x] = diag <= last ? bucket_of(a, diag - a.start) : -1;
-            __syncthreads();
-            if ((int)threadIdx.x < a.buckets)
-                for (int t = 0; t < kThreads; ++t)
-                    if (of[t] == (int)threadIdx.x) mine += sums[t];
+    const int heads = a.heads < 64 ? a.heads : 64, slots = 64 / heads, slot = lane / heads, width = c1 - c0, places = (r1 - r0) * width;
+    const float *dout = static_cast<const float *>(a.dout);
+    for (int h0 = 0; h0 < a.heads; h0 += heads) {
+        const int h = h0 + lane % heads;
+        float s = 0.f;
+        if (slot < slots && h < a.heads)
+            for (int p = slot; p < places; p += slots) {
+                const int r = p / width;
+                s += dout[((long)(r0 + r) * side + c0 + (p - r * width)) * a.heads + h];
+            }
+        lds[threadIdx.x] = s;
+        __syncthreads();
+        if (pair < B * B && lane < heads && h < a.heads) {
+            s = 0.f;
+            for (int i = 0; i < slots; ++i) s += lds[(wave << 6) + i * heads + lane];
+            float *out = a.dtable + (long)pair * a.heads + h;
+            *out = a.accumulate ? *out + s : s;
         }
-        if ((int)threadIdx.x < a.buckets) a.part[((long)h * a.slices + slice) * a.buckets + threadIdx.x] = mine;
         __syncthreads();
     }
 }
 
-__global__ __launch_bounds__(64) void sequence_sum_kernel(Args a)
-{
-    const int b = blockIdx.x, h = blockIdx.y;
-    double s = 0.;
-    for (long i = threadIdx.x; i < a.slices; i += 64) s += a.part[((long)h * a.slices + i) * a.buckets + b];
-#pragma unroll
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    if (threadIdx.x == 0) {
-        float *out = a.dtable + (long)b * a.heads + h;
-        *out = (float)(a.accumulate ? *out + s : s);
+// ---- the bias of a sequence -------------------------------------------------------------------------------------------------------
+// Bound by the writes of the bias.  out[h, i, j] depends on j - i: a tile of R rows and C columns has R + C - 1 different values, which go to LDS once
+// (a thread finds the bucket of its first offset and walks on from there).  A lane writes the same V columns of every row; from one row to the next its
+// values move up by one place, so a row costs a lane one value out of LDS, a shift of its vector and one wide store.
+
+template <typename T> struct Vector;
+template <> struct Vector<bf16_t> {
+    static constexpr int V = 8;
+    typedef uint16_t Bits;
+    uint4 w;
+    __device__ __forceinline__ void shift(uint32_t v)
+    {
+        w.w = __builtin_amdgcn_alignbit(w.w, w.z, 16);
+        w.z = __builtin_amdgcn_alignbit(w.z, w.y, 16);
+        w.y = __builtin_amdgcn_alignbit(w.y, w.x, 16);
+        w.x = w.x << 16 | v;
     }
+    __device__ __forceinline__ uint32_t at(int i) const
+    {
+        const uint32_t u = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
+        return i & 1 ? u >> 16 : u & 0xffffu;
+    }
+    static constexpr uint32_t kMinusInf = 0xff80u;
+};
+template <> struct Vector<float> {
+    static constexpr int V = 4;
+    typedef uint32_t Bits;
+    uint4 w;
+    __device__ __forceinline__ void shift(uint32_t v)
+    {
+        w.w = w.z;
+        w.z = w.y;
+        w.y = w.x;
+        w.x = v;
+    }
+    __device__ __forceinline__ uint32_t at(int i) const { return i < 2 ? (i ? w.y : w.x) : (i == 2 ? w.z : w.w); }
+    static constexpr uint32_t kMinusInf = 0xff800000u;
+};
+
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
+{
+    typedef Vector<T> Vec;
+    typedef typename Vec::Bits Bits;
+    constexpr int V = Vec::V, kColumns = THREADS * V;
+    __shared__ Bits values[kColumns + kMostFwdRows];
+    __shared__ Bits learned[2 * (RELPOS_MAX_EDGES + 1)];
+    __shared__ int edges[RELPOS_MAX_EDGES];
+    const int h = blockIdx.y;
+    for (int b = threadIdx.x; b < a.buckets; b += THREADS) learned[b] = static_cast<const Bits *>(a.table)[(long)b * a.heads + h];
+    for (int e = threadIdx.x; e < a.n; e += THREADS) edges[e] = a.edges[e];
+    const int tiles_k = (a.k + kColumns - 1) / kColumns;
+    const long tiles = (long)((a.q + a.rows - 1) / a.rows) * tiles_k;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int i0 = (int)(tile / tiles_k) * a.rows, j0 = (int)(tile % tiles_k) * kColumns;
+        const int i1 = i0 + a.rows < a.q ? i0 + a.rows : a.q, R = i1 - i0;
+        __syncthreads();
+        const int count = kColumns + R - 1, mine = (count + THREADS - 1) / THREADS, lowest = j0 - (i1 - 1) - a.start;
+        int n = -1;
+        for (int x = threadIdx.x * mine; x < (int)(threadIdx.x + 1) * mine && x < count; ++x) {
+            const int r = lowest + x, d = r < 0 ? -r : a.bidirectional ? r : 0;
+            if (n < 0) n = edges_up_to(edges, a.n, d);
+            while (n > 0 && edges[n - 1] > d) --n;
+            while (n < a.n && edges[n] <= d) ++n;
+            values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n + a.n + 1 : n];
+        }
+        __syncthreads();
+        const int c = threadIdx.x * V, j = j0 + c;
+        if (j < a.k) {
+            Vec v;
+#pragma unroll
+            for (int e = V - 1; e >= 0; --e) v.shift(values[c + R - 1 + e]);
+            Bits *row = static_cast<Bits *>(a.out) + ((long)h * a.q + i0) * a.ld + j;
+            if (j + V <= a.k) {
+#pragma unroll 4
+                for (int i = R - 1;; --i) {
+                    __builtin_memcpy(row, &v.w, 16);
+                    if (i == 0) break;
+                    row += a.ld;
+                    v.shift(values[c + i - 1]);
+                }
+            } else {
+                for (int i = R - 1;; --i) {
+#pragma unroll
+                    for (int e = 0; e < V - 1; ++e)
+                        if (j + e < a.k) row[e] = (Bits)v.at(e);
+                    if (i == 0) break;
+                    row += a.ld;
+                    v.shift(values[c + i - 1]);
+                }
+            }
+        }
+    }
+}
+
+// ---- its gradient -------------------------------------------------------------------------------------------------------------------
+// Bound by the reads of dout.  A wavefront takes kRows rows of 64 V columns, a lane V columns of every row, and keeps one sum for each of its
+// columns' diagonals (j - i = const: one offset, one bucket).  From one row to the next the sums move up by one place, from a lane's last to the next lane's
+// first; what leaves the last lane is the whole sum of a diagonal of this tile and waits in a lane of a register of its own.  So every value costs one
+// addition, in the same order every run, wherever its bucket's borders lie; only the 64 V + kRows - 1 sums of a tile are sorted into buckets, and most tiles
+// meet one bucket alone.
+
+// V columns of dout from column j on; zeros from column k on (k >= V: the vector that would reach over it is read V columns before it and moved)
+template <typename T, int V> struct Columns {
+    uint4 w;
+    __device__ __forceinline__ void load(const T *row, int j, int k, bool edge)
+    {
+        if constexpr (V == 1) {
+            w = make_uint4(0, 0, 0, 0);
+            if (j < k) w.x = sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t *>(row)[j] : reinterpret_cast<const uint32_t *>(row)[j];
+        } else {
+            __builtin_memcpy(&w, row + (j < k - V ? j : k - V), 16);
+            if (edge) {
+                const int cut = j + V - k; // columns too many
+                const int bits = cut > 0 ? (cut < V ? cut : V) * (int)(8 * sizeof(T)) : 0;
+                const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
+                const uint64_t l = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
+                const uint64_t u = bits < 64 ? hi >> bits : 0;
+                w = make_uint4((uint32_t)l, (uint32_t)(l >> 32), (uint32_t)u, (uint32_t)(u >> 32));
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        if constexpr (sizeof(T) == 4) return __uint_as_float(word[i]);
+        return i & 1 ? __uint_as_float(word[i / 2] & 0xffff0000u) : __uint_as_float(word[i / 2] << 16);
+    }
+};
+
+template <int CTRL> __device__ __forceinline__ float dpp_move(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v += dpp_move<0xB1>(v);
+    v += dpp_move<0x4E>(v);
+    v += dpp_move<0x141>(v);
+    v += dpp_move<0x140>(v);
+    return qgroup_sum(v);
+}
+
+template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequence_bwd_kernel(Args a)
+{
+    constexpr int kWaves = kThreads / 64, kColumns = 64 * V, kAtOnce = 8; // rows whose loads are in flight together
+    __shared__ float sums[kWaves][2 * (RELPOS_MAX_EDGES + 1)];
+    const int h = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int b = lane; b < a.buckets; b += 64) sums[wave][b] = 0.f;
+    __syncthreads();
+    const int tiles_q = (a.q + kRows - 1) / kRows, tiles_k = (a.k + kColumns * kWaves - 1) / (kColumns * kWaves);
+    const long tiles = (long)a.batch * tiles_q * tiles_k;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int tk = (int)(tile % tiles_k);
+        const long t = tile / tiles_k;
+        const int i0 = (int)(t % tiles_q) * kRows, b = (int)(t / tiles_q);
+        const int j0 = __builtin_amdgcn_readfirstlane((tk * kWaves + wave) * kColumns);
+        if (j0 >= a.k || (a.causal && j0 > i0 + kRows - 1 + a.start)) continue; // (nothing there, or nothing seen)
+        const T *rows = static_cast<const T *>(a.dout) + (((long)b * a.heads + h) * a.q + i0) * a.ld;
+        const int i1 = a.q - i0 < kRows ? a.q - i0 : kRows, j = j0 + lane * V;
+        const bool edge = j0 + kColumns > a.k;
+        float acc[V] = {}, gone = 0.f;
+        Columns<T, V> now[kAtOnce], next[kAtOnce];
+        const auto fetch = [&](int i, Columns<T, V> (&c)[kAtOnce]) {
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) {
+                c[r].w = make_uint4(0, 0, 0, 0);
+                // (a lane all of whose columns are hidden from these rows does without them)
+                if (i + r < i1 && !(a.causal && j > i0 + i + kAtOnce - 1 + a.start)) c[r].load(rows + (long)(i + r) * a.ld, j, a.k, edge);
+            }
+        };
+        fetch(0, now);
+        for (int i = 0; i < kRows; i += kAtOnce) {
+            if (i + kAtOnce < i1) fetch(i + kAtOnce, next);
+            else {
+#pragma unroll
+                for (int r = 0; r < kAtOnce; ++r) next[r].w = make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) {
+                if (i + r > 0) {
+                    const float out = acc[V - 1];
+                    // (wave_shl 1: what waits moves to the lane before, the last lane takes its own last sum)
+                    gone = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, out), __builtin_bit_cast(int, gone), 0x130, 0xF, 0xF,
+                                                                                 false));
+#pragma unroll
+                    for (int e = V - 1; e > 0; --e) acc[e] = acc[e - 1];
+                    acc[0] = dpp_move<0x138>(out); // (wave_shr 1: from the lane before; 0 into the first)
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += now[r].at(e);
+            }
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) now[r] = next[r];
+        }
+        // Sums by diagonal: acc[e] of offset j + e - (i0 + kRows - 1) - start, lane l > 0 of gone of (j0 + kColumns - 1) - (i0 + l - 1) - start.
+        const int low = j0 - (i0 + kRows - 1) - a.start, mine = low + lane * V, left = j0 + kColumns - i0 - a.start - lane;
+        const int high = j0 + kColumns - 1 - i0 - a.start, most = a.causal && high > 0 ? 0 : high;
+        int r = low, n = edges_up_to(a.edges, a.n, r <= 0 ? -r : a.bidirectional ? r : 0);
+        while (r <= most) { // runs of offsets of one bucket, from `r` to `end`
+            int end, bucket;
+            if (r <= 0 || !a.bidirectional) {
+                bucket = n;
+                end = n > 0 ? -a.edges[n - 1] : a.bidirectional ? 0 : most;
+            } else {
+                bucket = n + a.n + 1;
+                end = n < a.n ? a.edges[n] - 1 : most;
+            }
+            if (end >= r) {
+                float s = lane > 0 && left >= r && left <= end ? gone : 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) s += mine + e >= r && mine + e <= end ? acc[e] : 0.f;
+                s = wave_sum(s);
+                if (lane == 0) sums[wave][bucket] += s;
+            }
+            if (end >= most) break;
+            // on to the next run (equal edges: an empty one): nearer edges before the query, from none at all on farther ones behind it
+            if (r > 0) ++n;
+            else if (n > 0) --n;
+            r = end + 1 > r ? end + 1 : r;
+        }
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < a.buckets; b += kThreads)
+        a.part[((long)h * a.slices + blockIdx.x) * a.buckets + b] = (sums[0][b] + sums[1][b]) + (sums[2][b] + sums[3][b]);
+}
+
+// The workgroups' sums of a head: a thread per bucket and group of them, the groups in their order.
+__global__ __launch_bounds__(1024) void sequence_sum_kernel(Args a)
+{
+    __shared__ double lds[1024];
+    const int h = blockIdx.x, groups = 1024 / a.buckets, g = threadIdx.x / a.buckets, b = threadIdx.x - g * a.buckets;
+    double s = 0.;
+    if (g < groups)
+        for (int i = g; i < a.slices; i += groups) s += a.part[((long)h * a.slices + i) * a.buckets + b];
+    lds[threadIdx.x] = s;
+    __syncthreads();
+    if (g) return;
+    for (int i = 1; i < groups; ++i) s += lds[i * a.buckets + b];
+    float *out = a.dtable + (long)b * a.heads + h;
+    *out = (float)(a.accumulate ? *out + s : s);
 }
 
 struct Plan {
     size_t elem, out, dout, table, dtable, ws;
-    long ld, slices;
-    int buckets;
+    long ld;
+    int buckets, V;            // V: columns of a lane
+    bool narrow;               // workgroups of one wavefront for the bias
+    int rows; long fwd_tiles;  // rows of a tile of the bias, tiles of a head
+    int slices;
 };
+
+long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
 int make_plan(const relpos_desc *d, Plan *p)
 {
@@ -168,7 +388,19 @@ int make_plan(const relpos_desc *d, Plan *p)
         p->buckets = side;
         p->out = (((size_t)d->heads * d->q_len - 1) * p->ld + d->k_len) * p->elem;
         p->dout = (((size_t)rows * d->q_len - 1) * p->ld + d->k_len) * p->elem;
-        p->slices = (long)d->batch * ((d->q_len + kRows - 1) / kRows);
+        const int wide = (int)(16 / p->elem);
+        p->V = d->k_len < wide ? 1 : wide;
+        // The bias: as many rows a tile (64 at most, 8 at least) as leave 8 workgroups a compute unit, since a tile's values are found anew for each; where even
+        // 8 rows leave few, workgroups of one wavefront and a quarter of the columns.
+        const long across = ceil_div(d->k_len, (long)kThreads * wide) * d->heads;
+        p->narrow = across * ceil_div(d->q_len, 8) < 2 * kSizingCus;
+        p->rows = kMostFwdRows;
+        while (p->rows > 8 && across * ceil_div(d->q_len, p->rows) < 8 * kSizingCus) p->rows /= 2;
+        p->fwd_tiles = ceil_div(d->q_len, p->rows) * ceil_div(d->k_len, (long)(p->narrow ? 64 : kThreads) * wide);
+        // Its gradient: four workgroups a compute unit, over the heads, each with the same number of tiles if that comes out.
+        const long tiles = (long)d->batch * ceil_div(d->q_len, kRows) * ceil_div(d->k_len, (long)kThreads * p->V);
+        const long most = ceil_div(4 * kSizingCus, d->heads);
+        p->slices = (int)ceil_div(tiles, ceil_div(tiles, most < tiles ? most : tiles));
         p->ws = to_256((size_t)d->heads * p->slices * side * sizeof(float));
     }
     p->table = (size_t)p->buckets * d->heads * p->elem;
@@ -180,12 +412,24 @@ void fill(const relpos_desc *d, const Plan &p, Args *a)
 {
     *a = Args{};
     a->heads = d->heads; a->batch = d->batch; a->q = d->q_len; a->k = d->k_len; a->start = d->q_start;
-    a->window = d->window; a->buckets = p.buckets; a->ld = p.ld; a->slices = p.slices;
+    a->window = d->window; a->buckets = p.buckets; a->ld = p.ld; a->slices = p.slices; a->rows = p.rows;
     a->bidirectional = (d->flags & RELPOS_BIDIRECTIONAL) != 0;
     a->causal = (d->flags & RELPOS_CAUSAL) != 0;
     a->accumulate = (d->flags & RELPOS_ACCUM_WGRAD) != 0;
     a->n = d->n_edges;
     for (int i = 0; i < d->n_edges; ++i) a->edges[i] = d->edges[i];
+}
+
+template <typename T> void launch_forward(const Args &a, const Plan &p, dim3 grid, hipStream_t st)
+{
+    if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64>), grid, dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads>), grid, dim3(kThreads), 0, st, a);
+}
+
+template <typename T> void launch_backward(const Args &a, const Plan &p, dim3 grid, hipStream_t st)
+{
+    if (p.V == 1) hipLaunchKernelGGL((sequence_bwd_kernel<T, 1>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((sequence_bwd_kernel<T, 16 / sizeof(T)>), grid, dim3(kThreads), 0, st, a);
 }
 
 // base^n as a whole number of 32-bit digits, times another one
@@ -276,9 +520,9 @@ int relpos_forward(const relpos_desc *desc, const void *table, void *out, void *
         if (desc->dtype == GSWA_F32) hipLaunchKernelGGL(window_fwd_kernel<float>, grid, dim3(kThreads), 0, st, a);
         else hipLaunchKernelGGL(window_fwd_kernel<bf16_t>, grid, dim3(kThreads), 0, st, a);
     } else {
-        const dim3 grid(desc->q_len < 8192 ? desc->q_len : 8192, desc->heads);
-        if (desc->dtype == GSWA_F32) hipLaunchKernelGGL(sequence_fwd_kernel<float>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(sequence_fwd_kernel<bf16_t>, grid, dim3(kThreads), 0, st, a);
+        const dim3 grid((unsigned)(p.fwd_tiles < (1L << 20) ? p.fwd_tiles : 1L << 20), desc->heads);
+        if (desc->dtype == GSWA_F32) launch_forward<float>(a, p, grid, st);
+        else launch_forward<bf16_t>(a, p, grid, st);
     }
     RP_LAUNCHED();
     return GSWA_OK;
@@ -298,19 +542,19 @@ int relpos_backward(const relpos_desc *desc, const void *dout, float *dtable, vo
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (desc->window > 0) {
         KernelTimer t(K_RELPOS_BWD, st);
-        hipLaunchKernelGGL(window_bwd_kernel, dim3((unsigned)(((long)p.buckets * desc->heads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(window_bwd_kernel, dim3((p.buckets + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, st, a);
         RP_LAUNCHED();
         return GSWA_OK;
     }
-    const dim3 grid((unsigned)(p.slices < 65536 ? p.slices : 65536), desc->heads);
     {
         KernelTimer t(K_RELPOS_BWD, st);
-        if (desc->dtype == GSWA_F32) hipLaunchKernelGGL(sequence_bwd_kernel<float>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(sequence_bwd_kernel<bf16_t>, grid, dim3(kThreads), 0, st, a);
+        const dim3 grid(p.slices, desc->heads);
+        if (desc->dtype == GSWA_F32) launch_backward<float>(a, p, grid, st);
+        else launch_backward<bf16_t>(a, p, grid, st);
         RP_LAUNCHED();
     }
     KernelTimer t(K_RELPOS_SUM, st);
-    hipLaunchKernelGGL(sequence_sum_kernel, dim3(p.buckets, desc->heads), dim3(64), 0, st, a);
+    hipLaunchKernelGGL(sequence_sum_kernel, dim3(desc->heads), dim3(1024), 0, st, a);
     RP_LAUNCHED();
     return GSWA_OK;
 }

@@ -5,6 +5,8 @@ before the call; a missing library is an error, there is no fallback path.
 """
 import ctypes
 
+import torch
+
 from . import gswa
 from ._args import DTYPES, Call, torch_dtype
 from .gswa import _check
@@ -60,11 +62,10 @@ def lnorm_forward(desc, x, residual, gamma, beta, y, sum, stream=None):
 
 def lnorm_backward(desc, x, dy, gamma, dsum, dx, dgamma, dbeta, ws, stream=None):
     """gamma, dsum, and dgamma with dbeta (and then ws) may be None."""
-    import torch
     L, c = lib(), Call()
     t, rows, C = torch_dtype(desc.dtype), desc.rows, desc.C
     r = desc.r_stride or C
-    need = 0 if ws is None or isinstance(ws, int) else lnorm_query_bytes(desc)
+    need = lnorm_query_bytes(desc) if torch.is_tensor(ws) else 0
     c.run(L.lnorm_backward, stream, ctypes.byref(desc), c.rows("x", x, t, rows, C, desc.x_stride or C),
           c.rows("dy", dy, t, rows, C, desc.y_stride or C), c.flat("gamma", gamma, t, C), c.rows("dsum", dsum, t, rows, C, r),
           c.rows("dx", dx, t, rows, C, r), c.flat("dgamma", dgamma, torch.float32, C), c.flat("dbeta", dbeta, torch.float32, C),

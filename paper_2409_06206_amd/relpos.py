@@ -5,6 +5,8 @@ before the call; a missing library is an error, there is no fallback path.
 """
 import ctypes
 
+import torch
+
 from . import gswa
 from ._args import DTYPES, Call, torch_dtype
 from .gswa import _check
@@ -87,9 +89,8 @@ def relpos_forward(desc, table, out, stream=None):
 
 def relpos_backward(desc, dout, dtable, ws, stream=None):
     """ws may be None where relpos_query_bytes is 0."""
-    import torch
     L, c = lib(), Call()
-    need = 0 if ws is None or isinstance(ws, int) else relpos_query_bytes(desc)
+    need = relpos_query_bytes(desc) if torch.is_tensor(ws) else 0
     c.run(L.relpos_backward, stream, ctypes.byref(desc),
           _bias(c, "dout", dout, torch.float32 if desc.window else torch_dtype(desc.dtype), desc, desc.batch),
           c.flat("dtable", dtable, torch.float32, desc.buckets * desc.heads), c.flat("ws", ws, torch.uint8, need))

@@ -103,11 +103,11 @@ def test_plan_buffers_hold_a_line_per_tensor():
 def test_tensors_are_checked():
     p = torch.zeros(4)
     with pytest.raises(ValueError, match="GPU"):
-        adamw.adamw_query_bytes(adamw.make_desc(), [dict(p=p, g=p, m=p, v=p)])
+        adamw.adamw_plan(adamw.make_desc(), [dict(p=p, g=p, m=p, v=p)], None)
     with pytest.raises(ValueError, match="unknown"):
-        adamw.adamw_query_bytes(adamw.make_desc(), [dict(p=p, g=p, m=p, v=p, q=p)])
+        adamw.adamw_plan(adamw.make_desc(), [dict(p=p, g=p, m=p, v=p, q=p)], None)
     with pytest.raises(ValueError, match="gradients"):
-        adamw.adamw_query_bytes(adamw.make_desc(), [dict(p=p, g=p[:3], m=p, v=p)])
+        adamw.adamw_plan(adamw.make_desc(), [dict(p=p, g=p[:3], m=p, v=p)], None)
 
 
 def test_the_oracles_rounding_is_right_on_average_and_its_format_holds_what_it_rounds_to():
