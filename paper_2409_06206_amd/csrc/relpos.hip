@@ -39,7 +39,7 @@ template <typename E> __device__ __forceinline__ int edges_up_to(const E *edges,
 
 // ---- the table of a window --------------------------------------------------------------------------------------------------------
 // A few thousand values: what counts is the chain of dependent steps.  The buckets of the 2 M - 1 offsets of an axis are found side by side and kept
-// in LDS; a pair of buckets is a rectangle of offsets, which one wavefront sums.
+// in LDS; a pair of buckets is a rectangle of offsets, which one workgroup sums.
 
 template <typename T> __global__ __launch_bounds__(kThreads) void window_fwd_kernel(Args a)
 {
@@ -70,22 +70,20 @@ __device__ __forceinline__ void bucket_places(const Args &a, int b, int &lo, int
     if (first > last) lo = hi = 0;
 }
 
-// A wavefront per pair of buckets: its lanes take the heads of as many places at once as there is room for, places in their order; the lanes of a
-// head are summed in their order.
+// A workgroup per pair of buckets: its threads take the heads of as many places at once as there is room for, places in their order; the threads of
+// a head are summed in their order.
 __global__ __launch_bounds__(kThreads) void window_bwd_kernel(Args a)
 {
     __shared__ float lds[kThreads];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, B = 2 * (a.n + 1), side = 2 * a.window - 1;
-    const int pair = blockIdx.x * (kThreads / 64) + wave;
-    int r0 = 0, r1 = 0, c0 = 0, c1 = 0;
-    if (pair < B * B) {
-        bucket_places(a, pair / B, r0, r1);
-        bucket_places(a, pair % B, c0, c1);
-    }
-    const int heads = a.heads < 64 ? a.heads : 64, slots = 64 / heads, slot = lane / heads, width = c1 - c0, places = (r1 - r0) * width;
+    const int B = 2 * (a.n + 1), side = 2 * a.window - 1, pair = blockIdx.x;
+    int r0, r1, c0, c1;
+    bucket_places(a, pair / B, r0, r1);
+    bucket_places(a, pair % B, c0, c1);
+    const int heads = a.heads < kThreads ? a.heads : kThreads, width = c1 - c0, places = (r1 - r0) * width;
+    const int slots = kThreads / heads, slot = threadIdx.x / heads, used = slots < places ? slots : places;
     const float *dout = static_cast<const float *>(a.dout);
     for (int h0 = 0; h0 < a.heads; h0 += heads) {
-        const int h = h0 + lane % heads;
+        const int h = h0 + threadIdx.x % heads;
         float s = 0.f;
         if (slot < slots && h < a.heads)
             for (int p = slot; p < places; p += slots) {
@@ -94,9 +92,9 @@ __global__ __launch_bounds__(kThreads) void window_bwd_kernel(Args a)
             }
         lds[threadIdx.x] = s;
         __syncthreads();
-        if (pair < B * B && lane < heads && h < a.heads) {
+        if ((int)threadIdx.x < heads && h < a.heads) {
             s = 0.f;
-            for (int i = 0; i < slots; ++i) s += lds[(wave << 6) + i * heads + lane];
+            for (int i = 0; i < used; ++i) s += lds[i * heads + threadIdx.x];
             float *out = a.dtable + (long)pair * a.heads + h;
             *out = a.accumulate ? *out + s : s;
         }
@@ -126,6 +124,17 @@ template <> struct Vector<bf16_t> {
         const uint32_t u = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
         return i & 1 ? u >> 16 : u & 0xffffu;
     }
+    // 8 values from c + u on; c is a multiple of 8, values of 16, and u the same for all lanes
+    static __device__ __forceinline__ Vector from(const Bits *values, int c, int u)
+    {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(values) + c / 2 + u / 2;
+        const uint32_t x[5] = {p[0], p[1], p[2], p[3], p[4]};
+        Vector v;
+        v.w = u & 1 ? make_uint4(__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16),
+                                 __builtin_amdgcn_alignbit(x[4], x[3], 16))
+                    : make_uint4(x[0], x[1], x[2], x[3]);
+        return v;
+    }
     static constexpr uint32_t kMinusInf = 0xff80u;
 };
 template <> struct Vector<float> {
@@ -140,27 +149,37 @@ template <> struct Vector<float> {
         w.x = v;
     }
     __device__ __forceinline__ uint32_t at(int i) const { return i < 2 ? (i ? w.y : w.x) : (i == 2 ? w.z : w.w); }
+    static __device__ __forceinline__ Vector from(const Bits *values, int c, int u)
+    {
+        const uint32_t *p = values + c + u;
+        Vector v;
+        v.w = make_uint4(p[0], p[1], p[2], p[3]);
+        return v;
+    }
     static constexpr uint32_t kMinusInf = 0xff800000u;
 };
 
-template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
+// Rows that do not start at multiples of a 128-byte line: a wavefront's stores would cover lines in part (16 x 4096 x 4104: 3.8 TB/s, where 4096 columns reach
+// 5.6), so a lane's columns move with the row, back to the last line's start (m of them, the tile's ends with them), and its vector is read out of LDS
+// anew; elements before a row's first aligned vector and behind its last one are stored one by one.
+template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
 {
     typedef Vector<T> Vec;
     typedef typename Vec::Bits Bits;
-    constexpr int V = Vec::V, kColumns = THREADS * V;
-    __shared__ Bits values[kColumns + kMostFwdRows];
+    constexpr int V = Vec::V, kColumns = THREADS * V, kLine = 128 / sizeof(T), kBefore = ALIGNED ? 0 : kLine;
+    __shared__ __align__(16) Bits values[kColumns + kBefore + kMostFwdRows + 4];
     __shared__ Bits learned[2 * (RELPOS_MAX_EDGES + 1)];
     __shared__ int edges[RELPOS_MAX_EDGES];
     const int h = blockIdx.y;
     for (int b = threadIdx.x; b < a.buckets; b += THREADS) learned[b] = static_cast<const Bits *>(a.table)[(long)b * a.heads + h];
     for (int e = threadIdx.x; e < a.n; e += THREADS) edges[e] = a.edges[e];
-    const int tiles_k = (a.k + kColumns - 1) / kColumns;
+    const int tiles_k = (a.k + (ALIGNED ? 0 : kLine - 1) + kColumns - 1) / kColumns;
     const long tiles = (long)((a.q + a.rows - 1) / a.rows) * tiles_k;
     for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int i0 = (int)(tile / tiles_k) * a.rows, j0 = (int)(tile % tiles_k) * kColumns;
         const int i1 = i0 + a.rows < a.q ? i0 + a.rows : a.q, R = i1 - i0;
         __syncthreads();
-        const int count = kColumns + R - 1, mine = (count + THREADS - 1) / THREADS, lowest = j0 - (i1 - 1) - a.start;
+        const int count = kColumns + kBefore + R - 1, mine = (count + THREADS - 1) / THREADS, lowest = j0 - kBefore - (i1 - 1) - a.start;
         int n = -1;
         for (int x = threadIdx.x * mine; x < (int)(threadIdx.x + 1) * mine && x < count; ++x) {
             const int r = lowest + x, d = r < 0 ? -r : a.bidirectional ? r : 0;
@@ -170,12 +189,15 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void se
             values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n + a.n + 1 : n];
         }
         __syncthreads();
-        const int c = threadIdx.x * V, j = j0 + c;
-        if (j < a.k) {
+        const int c = threadIdx.x * V;
+        Bits *const first = static_cast<Bits *>(a.out) + ((long)h * a.q + i0) * a.ld + j0; // the tile's corner
+        if constexpr (ALIGNED) {
+            const int j = j0 + c;
+            if (j >= a.k) continue;
             Vec v;
 #pragma unroll
             for (int e = V - 1; e >= 0; --e) v.shift(values[c + R - 1 + e]);
-            Bits *row = static_cast<Bits *>(a.out) + ((long)h * a.q + i0) * a.ld + j;
+            Bits *row = first + c;
             if (j + V <= a.k) {
 #pragma unroll 4
                 for (int i = R - 1;; --i) {
@@ -192,6 +214,23 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void se
                     if (i == 0) break;
                     row += a.ld;
                     v.shift(values[c + i - 1]);
+                }
+            }
+        } else {
+#pragma unroll 2
+            for (int i = 0; i < R; ++i) {
+                Bits *row = first + (long)i * a.ld; // (of column j0, which is a multiple of a line)
+                const int m = (int)(reinterpret_cast<uintptr_t>(row) / sizeof(Bits)) & (kLine - 1), above = kLine + R - 1 - i;
+                const Vec v = Vec::from(values, c, above - m);
+                const int col = c - m;
+                if (j0 + col >= 0 && j0 + col + V <= a.k) *reinterpret_cast<uint4 *>(row + col) = v.w;
+                if (threadIdx.x < 2 * V) { // a lane an element
+                    const int o = m & (V - 1), head = threadIdx.x, last = ((a.k + o) & ~(V - 1)) - o - j0, tail = last + head - V;
+                    if (head < V) {
+                        if (j0 == 0 && o > 0 && head < V - o && head < a.k) row[head] = values[head + above];
+                    } else if (j0 + last >= 0 && last + m >= 0 && last + m < kColumns && j0 + tail < a.k) {
+                        row[tail] = values[tail + above];
+                    }
                 }
             }
         }
@@ -249,18 +288,20 @@ __device__ __forceinline__ float wave_sum(float v)
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequence_bwd_kernel(Args a)
 {
     constexpr int kWaves = kThreads / 64, kColumns = 64 * V, kAtOnce = 8; // rows whose loads are in flight together
+    constexpr int kLong = 48; // a run of more diagonals than this is summed by all lanes, a shorter one by one
     __shared__ float sums[kWaves][2 * (RELPOS_MAX_EDGES + 1)];
-    const int h = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ float diagonal[kWaves][kColumns + kRows];
+    __shared__ int edges[RELPOS_MAX_EDGES];
+    const int h = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int b = lane; b < a.buckets; b += 64) sums[wave][b] = 0.f;
+    for (int e = threadIdx.x; e < a.n; e += kThreads) edges[e] = a.edges[e];
     __syncthreads();
-    const int tiles_q = (a.q + kRows - 1) / kRows, tiles_k = (a.k + kColumns * kWaves - 1) / (kColumns * kWaves);
+    const int tiles_q = (a.q + kRows - 1) / kRows, tiles_k = (a.k + kColumns - 1) / kColumns;
     const long tiles = (long)a.batch * tiles_q * tiles_k;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int tk = (int)(tile % tiles_k);
+    for (long tile = (long)blockIdx.x * kWaves + wave; tile < tiles; tile += (long)gridDim.x * kWaves) {
         const long t = tile / tiles_k;
-        const int i0 = (int)(t % tiles_q) * kRows, b = (int)(t / tiles_q);
-        const int j0 = __builtin_amdgcn_readfirstlane((tk * kWaves + wave) * kColumns);
-        if (j0 >= a.k || (a.causal && j0 > i0 + kRows - 1 + a.start)) continue; // (nothing there, or nothing seen)
+        const int i0 = (int)(t % tiles_q) * kRows, b = (int)(t / tiles_q), j0 = (int)(tile % tiles_k) * kColumns;
+        if (a.causal && j0 > i0 + kRows - 1 + a.start) continue; // (nothing seen)
         const T *rows = static_cast<const T *>(a.dout) + (((long)b * a.heads + h) * a.q + i0) * a.ld;
         const int i1 = a.q - i0 < kRows ? a.q - i0 : kRows, j = j0 + lane * V;
         const bool edge = j0 + kColumns > a.k;
@@ -298,32 +339,44 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
 #pragma unroll
             for (int r = 0; r < kAtOnce; ++r) now[r] = next[r];
         }
-        // Sums by diagonal: acc[e] of offset j + e - (i0 + kRows - 1) - start, lane l > 0 of gone of (j0 + kColumns - 1) - (i0 + l - 1) - start.
-        const int low = j0 - (i0 + kRows - 1) - a.start, mine = low + lane * V, left = j0 + kColumns - i0 - a.start - lane;
-        const int high = j0 + kColumns - 1 - i0 - a.start, most = a.causal && high > 0 ? 0 : high;
-        int r = low, n = edges_up_to(a.edges, a.n, r <= 0 ? -r : a.bidirectional ? r : 0);
-        while (r <= most) { // runs of offsets of one bucket, from `r` to `end`
-            int end, bucket;
-            if (r <= 0 || !a.bidirectional) {
-                bucket = n;
-                end = n > 0 ? -a.edges[n - 1] : a.bidirectional ? 0 : most;
-            } else {
-                bucket = n + a.n + 1;
-                end = n < a.n ? a.edges[n] - 1 : most;
-            }
-            if (end >= r) {
-                float s = lane > 0 && left >= r && left <= end ? gone : 0.f;
+        // The sums in the order of their diagonals, from offset `low` on: acc[e] of a lane is (lane, e), and lane l > 0 of what has left is l from the end.
+        const int low = j0 - (i0 + kRows - 1) - a.start, high = j0 + kColumns - 1 - i0 - a.start, most = a.causal && high > 0 ? 0 : high;
+        float *diag = diagonal[wave];
 #pragma unroll
-                for (int e = 0; e < V; ++e) s += mine + e >= r && mine + e <= end ? acc[e] : 0.f;
-                s = wave_sum(s);
-                if (lane == 0) sums[wave][bucket] += s;
+        for (int e = 0; e < V; ++e) diag[lane * V + e] = acc[e];
+        if (lane > 0) diag[kColumns + kRows - 1 - lane] = gone;
+        __builtin_amdgcn_wave_barrier();
+        // A lane finds the offsets of its bucket among them, and sums them if they are few.
+        for (int b0 = 0; b0 < a.buckets; b0 += 64) {
+            const int bucket = b0 + lane, behind = bucket > a.n, n = behind ? bucket - a.n - 1 : bucket;
+            int from = 1, to = 0;
+            if (bucket < a.buckets) {
+                const int near = n ? edges[n - 1] : behind, far = n < a.n ? edges[n] - 1 : 0x7fffffff; // distances
+                from = behind ? near : -far;
+                to = behind ? far : !n && !a.bidirectional ? 0x7fffffff : -near;
+                from = (from > low ? from : low) - low;
+                to = (to < most ? to : most) - low;
             }
-            if (end >= most) break;
-            // on to the next run (equal edges: an empty one): nearer edges before the query, from none at all on farther ones behind it
-            if (r > 0) ++n;
-            else if (n > 0) --n;
-            r = end + 1 > r ? end + 1 : r;
+            const int length = to - from + 1;
+            if (length > 0 && length <= kLong) {
+                float s = 0.f;
+#pragma unroll 4
+                for (int x = from; x <= to; ++x) s += diag[x];
+                sums[wave][bucket] += s;
+            }
+            for (uint64_t left = __ballot(length > kLong); left; left &= left - 1) {
+                const int owner = __builtin_ctzll(left), first = __builtin_amdgcn_readlane(from, owner), last = __builtin_amdgcn_readlane(to, owner);
+                float s = 0.f;
+#pragma unroll
+                for (int x = 0; x < kColumns + kRows - 1; x += 64) {
+                    const int y = x + lane;
+                    s += y >= first && y <= last ? diag[y] : 0.f;
+                }
+                s = wave_sum(s);
+                if (lane == owner) sums[wave][bucket] += s;
+            }
         }
+        __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
     for (int b = threadIdx.x; b < a.buckets; b += kThreads)
@@ -351,7 +404,7 @@ struct Plan {
     long ld;
     int buckets, V;            // V: columns of a lane
     bool narrow;               // workgroups of one wavefront for the bias
-    int rows; long fwd_tiles;  // rows of a tile of the bias, tiles of a head
+    int rows;                  // of a tile of the bias
     int slices;
 };
 
@@ -393,14 +446,14 @@ int make_plan(const relpos_desc *d, Plan *p)
         // The bias: as many rows a tile (64 at most, 8 at least) as leave 8 workgroups a compute unit, since a tile's values are found anew for each; where even
         // 8 rows leave few, workgroups of one wavefront and a quarter of the columns.
         const long across = ceil_div(d->k_len, (long)kThreads * wide) * d->heads;
-        p->narrow = across * ceil_div(d->q_len, 8) < 2 * kSizingCus;
+        p->narrow = across * ceil_div(d->q_len, 8) < 2 * kSizingCus || d->k_len <= 64 * wide;
         p->rows = kMostFwdRows;
         while (p->rows > 8 && across * ceil_div(d->q_len, p->rows) < 8 * kSizingCus) p->rows /= 2;
-        p->fwd_tiles = ceil_div(d->q_len, p->rows) * ceil_div(d->k_len, (long)(p->narrow ? 64 : kThreads) * wide);
-        // Its gradient: four workgroups a compute unit, over the heads, each with the same number of tiles if that comes out.
-        const long tiles = (long)d->batch * ceil_div(d->q_len, kRows) * ceil_div(d->k_len, (long)kThreads * p->V);
-        const long most = ceil_div(4 * kSizingCus, d->heads);
-        p->slices = (int)ceil_div(tiles, ceil_div(tiles, most < tiles ? most : tiles));
+        // Its gradient: 16 workgroups a compute unit, over the heads, about three times what runs at once (tiles near the diagonal take longer, hidden ones no
+        // time).
+        const long tiles = ceil_div((long)d->batch * ceil_div(d->q_len, kRows) * ceil_div(d->k_len, 64L * p->V), kThreads / 64);
+        const long most = ceil_div(16 * kSizingCus, d->heads);
+        p->slices = (int)(most < tiles ? most : tiles);
         p->ws = to_256((size_t)d->heads * p->slices * side * sizeof(float));
     }
     p->table = (size_t)p->buckets * d->heads * p->elem;
@@ -420,10 +473,19 @@ void fill(const relpos_desc *d, const Plan &p, Args *a)
     for (int i = 0; i < d->n_edges; ++i) a->edges[i] = d->edges[i];
 }
 
-template <typename T> void launch_forward(const Args &a, const Plan &p, dim3 grid, hipStream_t st)
+template <typename T> void launch_forward(const Args &a, const Plan &p, hipStream_t st)
 {
-    if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64>), grid, dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads>), grid, dim3(kThreads), 0, st, a);
+    const int threads = p.narrow ? 64 : kThreads, line = 128 / (int)sizeof(T);
+    const bool aligned = p.ld % line == 0 && reinterpret_cast<uintptr_t>(a.out) % 128 == 0;
+    const long tiles = ceil_div(a.q, a.rows) * ceil_div((long)a.k + (aligned ? 0 : line - 1), threads * (16L / sizeof(T)));
+    const dim3 grid((unsigned)(tiles < (1L << 20) ? tiles : 1L << 20), a.heads);
+    if (aligned) {
+        if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64, true>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads, true>), grid, dim3(kThreads), 0, st, a);
+    } else {
+        if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64, false>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads, false>), grid, dim3(kThreads), 0, st, a);
+    }
 }
 
 template <typename T> void launch_backward(const Args &a, const Plan &p, dim3 grid, hipStream_t st)
@@ -520,9 +582,8 @@ int relpos_forward(const relpos_desc *desc, const void *table, void *out, void *
         if (desc->dtype == GSWA_F32) hipLaunchKernelGGL(window_fwd_kernel<float>, grid, dim3(kThreads), 0, st, a);
         else hipLaunchKernelGGL(window_fwd_kernel<bf16_t>, grid, dim3(kThreads), 0, st, a);
     } else {
-        const dim3 grid((unsigned)(p.fwd_tiles < (1L << 20) ? p.fwd_tiles : 1L << 20), desc->heads);
-        if (desc->dtype == GSWA_F32) launch_forward<float>(a, p, grid, st);
-        else launch_forward<bf16_t>(a, p, grid, st);
+        if (desc->dtype == GSWA_F32) launch_forward<float>(a, p, st);
+        else launch_forward<bf16_t>(a, p, st);
     }
     RP_LAUNCHED();
     return GSWA_OK;
@@ -542,7 +603,7 @@ int relpos_backward(const relpos_desc *desc, const void *dout, float *dtable, vo
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (desc->window > 0) {
         KernelTimer t(K_RELPOS_BWD, st);
-        hipLaunchKernelGGL(window_bwd_kernel, dim3((p.buckets + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(window_bwd_kernel, dim3(p.buckets), dim3(kThreads), 0, st, a);
         RP_LAUNCHED();
         return GSWA_OK;
     }
