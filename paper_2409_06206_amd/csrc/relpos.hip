@@ -12,7 +12,7 @@ namespace gswa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 64;         // rows of a tile of the gradient, one lane of the values that leave it each
+constexpr int kMostRows = 32;     // rows of a tile of the gradient, at most (64 lanes hold what leaves it)
 constexpr int kMostFwdRows = 64;  // rows of a tile of the bias, at most
 
 struct Args {
@@ -21,7 +21,8 @@ struct Args {
     float *dtable, *part; // part: [heads][slices][buckets]
     long ld;
     int heads, batch, q, k, start, window, buckets, bidirectional, causal, accumulate, n;
-    int rows, slices;     // rows of a tile of the bias; workgroups of a head in the sums of the gradient
+    int rows, grad_rows;  // of a tile of the bias and of the gradient
+    int slices;           // workgroups of a head in the sums of the gradient
     int edges[RELPOS_MAX_EDGES];
 };
 
@@ -238,11 +239,11 @@ template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(TH
 }
 
 // ---- its gradient -------------------------------------------------------------------------------------------------------------------
-// Bound by the reads of dout.  A wavefront takes kRows rows of 64 V columns, a lane V columns of every row, and keeps one sum for each of its
+// Bound by the reads of dout.  A wavefront takes 8 to 32 rows of 64 V columns, a lane V columns of every row, and keeps one sum for each of its
 // columns' diagonals (j - i = const: one offset, one bucket).  From one row to the next the sums move up by one place, from a lane's last to the next lane's
 // first; what leaves the last lane is the whole sum of a diagonal of this tile and waits in a lane of a register of its own.  So every value costs one
-// addition, in the same order every run, wherever its bucket's borders lie; only the 64 V + kRows - 1 sums of a tile are sorted into buckets, and most tiles
-// meet one bucket alone.
+// addition, in the same order every run, wherever its bucket's borders lie; only the sums of a tile's diagonals, some 64 V, are sorted into buckets, and most
+// tiles meet one bucket alone.
 
 // V columns of dout from column j on; zeros from column k on (k >= V: the vector that would reach over it is read V columns before it and moved)
 template <typename T, int V> struct Columns {
@@ -287,23 +288,23 @@ __device__ __forceinline__ float wave_sum(float v)
 
 template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequence_bwd_kernel(Args a)
 {
-    constexpr int kWaves = kThreads / 64, kColumns = 64 * V, kAtOnce = 8; // rows whose loads are in flight together
+    constexpr int kWaves = kThreads / 64, kColumns = 64 * V, kAtOnce = 4; // rows whose loads are in flight together
     constexpr int kLong = 48; // a run of more diagonals than this is summed by all lanes, a shorter one by one
     __shared__ float sums[kWaves][2 * (RELPOS_MAX_EDGES + 1)];
-    __shared__ float diagonal[kWaves][kColumns + kRows];
+    __shared__ float diagonal[kWaves][kColumns + 64];
     __shared__ int edges[RELPOS_MAX_EDGES];
     const int h = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int b = lane; b < a.buckets; b += 64) sums[wave][b] = 0.f;
     for (int e = threadIdx.x; e < a.n; e += kThreads) edges[e] = a.edges[e];
     __syncthreads();
-    const int tiles_q = (a.q + kRows - 1) / kRows, tiles_k = (a.k + kColumns - 1) / kColumns;
+    const int R = a.grad_rows, tiles_q = (a.q + R - 1) / R, tiles_k = (a.k + kColumns - 1) / kColumns;
     const long tiles = (long)a.batch * tiles_q * tiles_k;
     for (long tile = (long)blockIdx.x * kWaves + wave; tile < tiles; tile += (long)gridDim.x * kWaves) {
         const long t = tile / tiles_k;
-        const int i0 = (int)(t % tiles_q) * kRows, b = (int)(t / tiles_q), j0 = (int)(tile % tiles_k) * kColumns;
-        if (a.causal && j0 > i0 + kRows - 1 + a.start) continue; // (nothing seen)
+        const int i0 = (int)(t % tiles_q) * R, b = (int)(t / tiles_q), j0 = (int)(tile % tiles_k) * kColumns;
+        if (a.causal && j0 > i0 + R - 1 + a.start) continue; // (nothing seen)
         const T *rows = static_cast<const T *>(a.dout) + (((long)b * a.heads + h) * a.q + i0) * a.ld;
-        const int i1 = a.q - i0 < kRows ? a.q - i0 : kRows, j = j0 + lane * V;
+        const int i1 = a.q - i0 < R ? a.q - i0 : R, j = j0 + lane * V;
         const bool edge = j0 + kColumns > a.k;
         float acc[V] = {}, gone = 0.f;
         Columns<T, V> now[kAtOnce], next[kAtOnce];
@@ -316,7 +317,7 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
             }
         };
         fetch(0, now);
-        for (int i = 0; i < kRows; i += kAtOnce) {
+        for (int i = 0; i < R; i += kAtOnce) {
             if (i + kAtOnce < i1) fetch(i + kAtOnce, next);
             else {
 #pragma unroll
@@ -339,12 +340,13 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
 #pragma unroll
             for (int r = 0; r < kAtOnce; ++r) now[r] = next[r];
         }
-        // The sums in the order of their diagonals, from offset `low` on: acc[e] of a lane is (lane, e), and lane l > 0 of what has left is l from the end.
-        const int low = j0 - (i0 + kRows - 1) - a.start, high = j0 + kColumns - 1 - i0 - a.start, most = a.causal && high > 0 ? 0 : high;
+        // The sums in the order of their diagonals, from offset `low` on: acc[e] of a lane is (lane, e), and what has left stands in the last
+        // R - 1 lanes, the farthest offset first.
+        const int low = j0 - (i0 + R - 1) - a.start, high = j0 + kColumns - 1 - i0 - a.start, most = a.causal && high > 0 ? 0 : high;
         float *diag = diagonal[wave];
 #pragma unroll
         for (int e = 0; e < V; ++e) diag[lane * V + e] = acc[e];
-        if (lane > 0) diag[kColumns + kRows - 1 - lane] = gone;
+        if (lane > 64 - R) diag[kColumns + 63 - lane] = gone;
         __builtin_amdgcn_wave_barrier();
         // A lane finds the offsets of its bucket among them, and sums them if they are few.
         for (int b0 = 0; b0 < a.buckets; b0 += 64) {
@@ -368,7 +370,7 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
                 const int owner = __builtin_ctzll(left), first = __builtin_amdgcn_readlane(from, owner), last = __builtin_amdgcn_readlane(to, owner);
                 float s = 0.f;
 #pragma unroll
-                for (int x = 0; x < kColumns + kRows - 1; x += 64) {
+                for (int x = 0; x < kColumns + kMostRows - 1; x += 64) {
                     const int y = x + lane;
                     s += y >= first && y <= last ? diag[y] : 0.f;
                 }
@@ -404,7 +406,7 @@ struct Plan {
     long ld;
     int buckets, V;            // V: columns of a lane
     bool narrow;               // workgroups of one wavefront for the bias
-    int rows;                  // of a tile of the bias
+    int rows, grad_rows;       // of a tile of the bias and of the gradient
     int slices;
 };
 
@@ -449,9 +451,12 @@ int make_plan(const relpos_desc *d, Plan *p)
         p->narrow = across * ceil_div(d->q_len, 8) < 2 * kSizingCus || d->k_len <= 64 * wide;
         p->rows = kMostFwdRows;
         while (p->rows > 8 && across * ceil_div(d->q_len, p->rows) < 8 * kSizingCus) p->rows /= 2;
-        // Its gradient: 16 workgroups a compute unit, over the heads, about three times what runs at once (tiles near the diagonal take longer, hidden ones no
-        // time).
-        const long tiles = ceil_div((long)d->batch * ceil_div(d->q_len, kRows) * ceil_div(d->k_len, 64L * p->V), kThreads / 64);
+        // Its gradient: tiles of 32 rows, fewer where that leaves less than four a compute unit; 16 workgroups a compute unit, over the
+        // heads, more than run at once (tiles near the diagonal take longer, hidden ones no time).
+        const long images = (long)d->batch * ceil_div(d->k_len, 64L * p->V);
+        p->grad_rows = kMostRows;
+        while (p->grad_rows > 8 && images * d->heads * ceil_div(d->q_len, p->grad_rows) < 4 * kSizingCus) p->grad_rows /= 2;
+        const long tiles = ceil_div(images * ceil_div(d->q_len, p->grad_rows), kThreads / 64);
         const long most = ceil_div(16 * kSizingCus, d->heads);
         p->slices = (int)(most < tiles ? most : tiles);
         p->ws = to_256((size_t)d->heads * p->slices * side * sizeof(float));
@@ -465,7 +470,7 @@ void fill(const relpos_desc *d, const Plan &p, Args *a)
 {
     *a = Args{};
     a->heads = d->heads; a->batch = d->batch; a->q = d->q_len; a->k = d->k_len; a->start = d->q_start;
-    a->window = d->window; a->buckets = p.buckets; a->ld = p.ld; a->slices = p.slices; a->rows = p.rows;
+    a->window = d->window; a->buckets = p.buckets; a->ld = p.ld; a->slices = p.slices; a->rows = p.rows; a->grad_rows = p.grad_rows;
     a->bidirectional = (d->flags & RELPOS_BIDIRECTIONAL) != 0;
     a->causal = (d->flags & RELPOS_CAUSAL) != 0;
     a->accumulate = (d->flags & RELPOS_ACCUM_WGRAD) != 0;
