@@ -13,8 +13,9 @@ namespace gswa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlock = 256;             // elements that share an exponent
-constexpr int kChunkBlocks = 8;         // blocks of one piece of work
+constexpr int kWaves = kThreads / 64;
+constexpr int kBlock = 256;             // elements that share an exponent: four for each lane of a wavefront
+constexpr int kChunkBlocks = 8;         // blocks of one piece of work: two for each wavefront of a workgroup
 constexpr long kChunk = (long)kBlock * kChunkBlocks;
 constexpr int kNormBlocks = 1024;
 
@@ -92,49 +93,81 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
     return x ^ x >> 16;
 }
 
-__device__ __forceinline__ float grad(const Tensor &t, long i)
+// A lane's four elements of a block, from `i` on, as many of them as the tensor has; a whole four by one wide access.
+template <typename T> __device__ __forceinline__ void load4(const T *p, int left, T (&v)[4])
 {
-    return t.g_bf16 ? to_f32(static_cast<const bf16_t *>(t.g)[i]) : static_cast<const float *>(t.g)[i];
+    if (left >= 4) {
+        __builtin_memcpy(v, __builtin_assume_aligned(p, 4 * sizeof(T) < 16 ? 4 * sizeof(T) : 16), 4 * sizeof(T));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < left ? p[j] : T{};
+    }
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, int left, const T (&v)[4])
+{
+    if (left >= 4) {
+        __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(T) < 16 ? 4 * sizeof(T) : 16), v, 4 * sizeof(T));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) p[j] = v[j];
+    }
+}
+// (bf16 or fp32 by a flag of the tensor, the same for a whole wavefront)
+__device__ __forceinline__ void load4_as(const void *p, long i, bool bf16, int left, float (&f)[4])
+{
+    if (bf16) {
+        bf16_t v[4];
+        load4(static_cast<const bf16_t *>(p) + i, left, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = to_f32(v[j]);
+    } else {
+        load4(static_cast<const float *>(p) + i, left, f);
+    }
 }
 
 // a wavefront's largest pattern
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t v)
+{
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+    return o > v ? o : v;
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-#pragma unroll
-    for (int s = 32; s; s >>= 1) {
-        const uint32_t o = __shfl_xor(v, s);
-        v = o > v ? o : v;
-    }
-    return v;
+    v = dpp_max<0xB1>(v);
+    v = dpp_max<0x4E>(v);
+    v = dpp_max<0x141>(v);
+    v = dpp_max<0x140>(v);
+    u32x2 r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = r[0] > r[1] ? r[0] : r[1];
+    r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return r[0] > r[1] ? r[0] : r[1];
 }
 
-// value of code c (without its sign) in a block of exponent E
-__device__ __forceinline__ float decode(uint32_t c, uint32_t E, int top)
+// Value of code c (without its sign) in a block of exponent E, and the code of a magnitude's pattern rounded by 16 random bits.
+template <int TOP> __device__ __forceinline__ float decode(uint32_t c, int E)
 {
-    if (E == 255) return __uint_as_float(0x7fc00000u);
-    const int T = (int)(8 * (E + 1)) - top + (int)c;
-    return c ? __uint_as_float((uint32_t)(T > 1 ? T : 1) << 20) : 0.f;
+    const int T = 8 * (E + 1) - TOP + (int)c;
+    const uint32_t bits = c ? (uint32_t)(T > 1 ? T : 1) << 20 : 0u;
+    return __uint_as_float(E == 255 ? 0x7fc00000u : bits);
 }
-
-// code of a magnitude's pattern, rounded by 16 random bits
-__device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t E, uint32_t noise, int top)
+template <int TOP> __device__ __forceinline__ uint32_t encode(uint32_t bits, int E, uint32_t noise)
 {
-    if (E == 255) return 0;
+    constexpr int least = TOP == 255 ? 1 : 0; // (a second moment that is not 0 is not stored as 0)
     int T = (int)((bits + (noise << 4)) >> 20);
-    const bool signless = top == 255;
-    if (signless ? bits == 0 : T < 1) return 0;
-    if (T < 1) T = 1;
-    int c = T - ((int)(8 * (E + 1)) - top);
-    if (c < (int)signless) c = signless;
-    const int most = E == 254 ? top - 1 : top;
-    return (uint32_t)(c < most ? c : most);
+    const bool none = least ? bits == 0 : T < 1;
+    T = T > 1 ? T : 1;
+    const int c = T - (8 * (E + 1) - TOP), most = E == 254 ? TOP - 1 : TOP;
+    return none || E == 255 ? 0u : (uint32_t)(c < least ? least : c > most ? most : c);
 }
 
-// A wavefront takes one block at a time, four elements a lane.
-__global__ __launch_bounds__(kThreads) void step_kernel(Step a)
+// What a step needs of its number and rates, the same for all elements.
+struct Rates {
+    float lr, rate, root, clip; // learning rate; over 1 - beta1^t; sqrt(1 - beta2^t); factor of the gradients
+    uint32_t key;
+};
+__device__ __forceinline__ Rates rates_of(const Step &a, float norm)
 {
-    const float norm = a.norm ? *a.norm : 0.f;
-    if (a.skip && !(fabsf(norm) < INFINITY)) return;
     const uint64_t t = (uint64_t)*a.step + 1;
     double b1 = 1., b2 = 1., f1 = a.beta1, f2 = a.beta2; // beta^t by squares
     for (uint64_t e = t; e; e >>= 1) {
@@ -142,74 +175,122 @@ __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
         f1 *= f1;
         f2 *= f2;
     }
-    const float lr = a.lr_scale ? a.lr * *a.lr_scale : a.lr;
-    const float rate = lr / (float)(1. - b1), root = sqrtf((float)(1. - b2));
-    const float clip = a.max_norm > 0.f && norm > a.max_norm ? a.max_norm / norm : 1.f;
-    uint32_t key = mix(mix(a.seed_hi ^ 0x510E527Fu) ^ a.seed_lo);
-    key = mix(mix(key ^ (uint32_t)(t >> 32)) ^ (uint32_t)t);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    Rates r;
+    r.lr = a.lr_scale ? a.lr * *a.lr_scale : a.lr;
+    r.rate = r.lr / (float)(1. - b1);
+    r.root = sqrtf((float)(1. - b2));
+    r.clip = a.max_norm > 0.f && norm > a.max_norm ? a.max_norm / norm : 1.f;
+    r.key = mix(mix(a.seed_hi ^ 0x510E527Fu) ^ a.seed_lo);
+    r.key = mix(mix(r.key ^ (uint32_t)(t >> 32)) ^ (uint32_t)t);
+    return r;
+}
+
+// What the next step sees of the states is rounded from m' and v', so these are formed by products and sums that are rounded one by one
+// (no fused multiply-add): the result does not hang on how a compiler joins them.
+__device__ __forceinline__ void moments(const Step &a, float g, float &m, float &v)
+{
+#pragma clang fp contract(off)
+    m = m * a.b1 + g * a.b1c;
+    v = v * a.b2 + g * g * a.b2c;
+}
+
+// Bound by memory: 16 to 30 bytes an element against some 40 operations.  A workgroup takes pieces of 8 blocks, a wavefront two of them with all loads of both
+// in flight together; a block's largest magnitude comes from exchanges between its lanes.
+template <bool EIGHT> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
+{
+    constexpr int kEach = kChunkBlocks / kWaves;
+    const float norm = a.norm ? *a.norm : 0.f;
+    if (a.skip && !(fabsf(norm) < INFINITY)) return;
+    const Rates r = rates_of(a, norm);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-        const Tensor &T = a.tensors[a.owner[chunk]];
-        const long c = chunk - T.first_chunk;
-        for (int b = wave; b < kChunkBlocks; b += kThreads / 64) {
-            const long block = c * kChunkBlocks + b, i0 = block * kBlock + lane * 4;
-            if (block * kBlock >= T.n) break;
-            const uint64_t number = (uint64_t)(T.first_block + block) * kBlock + lane * 4;
-            const uint32_t k = mix(key ^ (uint32_t)(number >> 32));
-            float m[4], v[4];
+        const Tensor T = a.tensors[a.owner[chunk]];
+        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
+        float g[kEach][4], p[kEach][4], m[kEach][4], v[kEach][4];
+        uint8_t cm[kEach][4], cv[kEach][4];
+        int em[kEach], ev[kEach], left[kEach];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const long block = first + k * kWaves, i = block * kBlock + lane * 4, n = T.n - i;
+            left[k] = n < 0 ? 0 : n < 4 ? (int)n : 4;
+            if (block * kBlock >= T.n) continue;
+            load4_as(T.g, i, T.g_bf16, left[k], g[k]);
+            if (T.master) load4(T.master + i, left[k], p[k]);
+            else load4_as(T.p, i, T.p_bf16, left[k], p[k]);
+            if (EIGHT) {
+                load4(static_cast<const uint8_t *>(T.m) + i, left[k], cm[k]);
+                load4(static_cast<const uint8_t *>(T.v) + i, left[k], cv[k]);
+                em[k] = T.m_exp[block];
+                ev[k] = T.v_exp[block];
+            } else {
+                load4(static_cast<const float *>(T.m) + i, left[k], m[k]);
+                load4(static_cast<const float *>(T.v) + i, left[k], v[k]);
+            }
+        }
+        const float keep = 1.f - r.lr * T.decay;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const long block = first + k * kWaves, i = block * kBlock + lane * 4;
+            if (block * kBlock >= T.n) continue;
             uint32_t mmax = 0, vmax = 0;
+#pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const long i = i0 + j;
-                m[j] = v[j] = 0.f;
-                if (i >= T.n) continue;
-                if (a.eight) {
-                    const uint32_t cm = static_cast<const uint8_t *>(T.m)[i], cv = static_cast<const uint8_t *>(T.v)[i];
-                    m[j] = decode(cm & 127, T.m_exp[block], 127);
-                    if (cm & 128) m[j] = -m[j];
-                    v[j] = decode(cv, T.v_exp[block], 255);
-                } else {
-                    m[j] = static_cast<const float *>(T.m)[i];
-                    v[j] = static_cast<const float *>(T.v)[i];
+                if (EIGHT) {
+                    m[k][j] = decode<127>(cm[k][j] & 127, em[k]);
+                    if (cm[k][j] & 128) m[k][j] = -m[k][j];
+                    v[k][j] = decode<255>(cv[k][j], ev[k]);
                 }
-                const float g = grad(T, i) * clip;
-                m[j] = a.b1 * m[j] + a.b1c * g;
-                v[j] = a.b2 * v[j] + a.b2c * (g * g);
-                float p = T.master ? T.master[i] : T.p_bf16 ? to_f32(static_cast<const bf16_t *>(T.p)[i]) : static_cast<const float *>(T.p)[i];
-                p = p * (1.f - lr * T.decay) - rate * m[j] / (sqrtf(v[j]) / root + a.eps);
-                if (T.master) {
-                    T.master[i] = p;
-                    from_f32(static_cast<bf16_t *>(T.p)[i], p);
-                } else if (T.p_bf16) {
-                    uint32_t bits = __float_as_uint(p);
-                    if ((bits & 0x7f800000u) != 0x7f800000u) bits += mix(mix((uint32_t)(number + j) ^ k) ^ 0xBB67AE85u) & 0xffffu;
-                    static_cast<bf16_t *>(T.p)[i].bits = (uint16_t)(bits >> 16);
-                    if (p != p) static_cast<bf16_t *>(T.p)[i].bits = 0x7fc0u;
-                } else {
-                    static_cast<float *>(T.p)[i] = p;
+                moments(a, g[k][j] * r.clip, m[k][j], v[k][j]);
+                p[k][j] = p[k][j] * keep - r.rate * m[k][j] / (sqrtf(v[k][j]) / r.root + a.eps);
+                if (EIGHT && j < left[k]) {
+                    const uint32_t mb = __float_as_uint(m[k][j]) & 0x7fffffffu, vb = __float_as_uint(v[k][j]) & 0x7fffffffu;
+                    mmax = mb > mmax ? mb : mmax;
+                    vmax = vb > vmax ? vb : vmax;
                 }
-                const uint32_t mb = __float_as_uint(m[j]) & 0x7fffffffu, vb = __float_as_uint(v[j]) & 0x7fffffffu;
-                mmax = mb > mmax ? mb : mmax;
-                vmax = vb > vmax ? vb : vmax;
             }
-            if (!a.eight) {
-                for (int j = 0; j < 4; ++j)
-                    if (i0 + j < T.n) {
-                        static_cast<float *>(T.m)[i0 + j] = m[j];
-                        static_cast<float *>(T.v)[i0 + j] = v[j];
+            const uint64_t number = (uint64_t)(T.first_block + block) * kBlock + lane * 4;
+            uint32_t h[4];
+            const bool noisy = T.p_bf16 && !T.master;
+            if (EIGHT || noisy) {
+                const uint32_t key = mix(r.key ^ (uint32_t)(number >> 32));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[j] = mix(((uint32_t)number + j) ^ key);
+            }
+            if (T.p_bf16) {
+                bf16_t q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (noisy) {
+                        uint32_t bits = __float_as_uint(p[k][j]);
+                        if ((bits & 0x7f800000u) != 0x7f800000u) bits += mix(h[j] ^ 0xBB67AE85u) & 0xffffu;
+                        q[j].bits = p[k][j] == p[k][j] ? (uint16_t)(bits >> 16) : (uint16_t)0x7fc0;
+                    } else {
+                        from_f32(q[j], p[k][j]);
                     }
-                continue;
+                }
+                store4(static_cast<bf16_t *>(T.p) + i, left[k], q);
+                if (T.master) store4(T.master + i, left[k], p[k]);
+            } else {
+                store4(static_cast<float *>(T.p) + i, left[k], p[k]);
             }
-            const uint32_t Em = wave_max(mmax) >> 23, Ev = wave_max(vmax) >> 23;
-            if (lane == 0) {
-                T.m_exp[block] = (uint8_t)Em;
-                T.v_exp[block] = (uint8_t)Ev;
-            }
-            for (int j = 0; j < 4; ++j) {
-                if (i0 + j >= T.n) break;
-                const uint32_t h = mix((uint32_t)(number + j) ^ k), mb = __float_as_uint(m[j]);
-                const uint32_t cm = encode(mb & 0x7fffffffu, Em, h & 0xffffu, 127);
-                static_cast<uint8_t *>(T.m)[i0 + j] = (uint8_t)(cm | (cm ? mb >> 24 & 128u : 0u));
-                static_cast<uint8_t *>(T.v)[i0 + j] = (uint8_t)encode(__float_as_uint(v[j]) & 0x7fffffffu, Ev, h >> 16, 255);
+            if (EIGHT) {
+                const int Em = (int)(wave_max(mmax) >> 23), Ev = (int)(wave_max(vmax) >> 23);
+                if (lane == 0) {
+                    T.m_exp[block] = (uint8_t)Em;
+                    T.v_exp[block] = (uint8_t)Ev;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t mb = __float_as_uint(m[k][j]);
+                    const uint32_t c = encode<127>(mb & 0x7fffffffu, Em, h[j] & 0xffffu);
+                    cm[k][j] = (uint8_t)(c | (c ? mb >> 24 & 128u : 0u));
+                    cv[k][j] = (uint8_t)encode<255>(__float_as_uint(v[k][j]) & 0x7fffffffu, Ev, h[j] >> 16);
+                }
+                store4(static_cast<uint8_t *>(T.m) + i, left[k], cm[k]);
+                store4(static_cast<uint8_t *>(T.v) + i, left[k], cv[k]);
+            } else {
+                store4(static_cast<float *>(T.m) + i, left[k], m[k]);
+                store4(static_cast<float *>(T.v) + i, left[k], v[k]);
             }
         }
     }
@@ -222,21 +303,30 @@ __global__ void count_kernel(Step a)
     *a.step += 1;
 }
 
+// Squares are summed in fp64, which costs nothing beside the reads: no gradient's square overflows or is lost.
 __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
 {
-    __shared__ double lds[kThreads / 64];
+    constexpr int kEach = kChunkBlocks / kWaves;
+    __shared__ double lds[kWaves];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     double s = 0.;
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-        const Tensor &T = a.tensors[a.owner[chunk]];
-        const long i0 = (chunk - T.first_chunk) * kChunk, i1 = i0 + kChunk < T.n ? i0 + kChunk : T.n;
-        for (long i = i0 + threadIdx.x; i < i1; i += kThreads) {
-            const double g = grad(T, i);
-            s += g * g;
+        const Tensor T = a.tensors[a.owner[chunk]];
+        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
+        float g[kEach][4];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const long i = (first + k * kWaves) * kBlock + lane * 4, n = T.n - i;
+            load4_as(T.g, i, T.g_bf16, n < 0 ? 0 : n < 4 ? (int)n : 4, g[k]);
         }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += (double)g[k][j] * (double)g[k][j];
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    if (lane == 0) lds[wave] = s;
     __syncthreads();
     if (threadIdx.x == 0) a.part[blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
@@ -252,19 +342,27 @@ __global__ __launch_bounds__(64) void norm_sum_kernel(Step a, int parts)
 
 __global__ __launch_bounds__(kThreads) void unpack_kernel(Step a)
 {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-        const Tensor &T = a.tensors[a.owner[chunk]];
-        const long i0 = (chunk - T.first_chunk) * kChunk, end = (T.n + kBlock - 1) / kBlock * kBlock;
-        for (long i = i0 + threadIdx.x; i < end && i < i0 + kChunk; i += kThreads) {
-            const long at = T.first_block * kBlock + i;
-            uint16_t m = 0, v = 0;
-            if (i < T.n) {
-                const uint32_t cm = static_cast<const uint8_t *>(T.m)[i], cv = static_cast<const uint8_t *>(T.v)[i];
-                m = (uint16_t)(__float_as_uint(decode(cm & 127, T.m_exp[i / kBlock], 127)) >> 16 | (cm & 128) << 8);
-                v = (uint16_t)(__float_as_uint(decode(cv, T.v_exp[i / kBlock], 255)) >> 16);
+        const Tensor T = a.tensors[a.owner[chunk]];
+        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
+#pragma unroll
+        for (int k = 0; k < kChunkBlocks / kWaves; ++k) {
+            const long block = first + k * kWaves, i = block * kBlock + lane * 4, n = T.n - i, at = T.first_block * kBlock + i;
+            if (block * kBlock >= T.n) break;
+            const int left = n < 0 ? 0 : n < 4 ? (int)n : 4;
+            uint8_t cm[4] = {}, cv[4] = {};
+            if (a.m_out) load4(static_cast<const uint8_t *>(T.m) + i, left, cm);
+            if (a.v_out) load4(static_cast<const uint8_t *>(T.v) + i, left, cv);
+            const int em = T.m_exp[block], ev = T.v_exp[block];
+            uint16_t m[4], v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { // (zeros behind the tensor's end)
+                m[j] = j < left ? (uint16_t)(__float_as_uint(decode<127>(cm[j] & 127, em)) >> 16 | (cm[j] & 128) << 8) : 0;
+                v[j] = j < left ? (uint16_t)(__float_as_uint(decode<255>(cv[j], ev)) >> 16) : 0;
             }
-            if (a.m_out) a.m_out[at] = m;
-            if (a.v_out) a.v_out[at] = v;
+            if (a.m_out) store4(a.m_out + at, 4, m);
+            if (a.v_out) store4(a.v_out + at, 4, v);
         }
     }
 }
@@ -458,7 +556,9 @@ int adamw_step(const adamw_plan_t *plan, int64_t *step, float lr, const float *l
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_STEP, st);
     if (plan->chunks) {
-        hipLaunchKernelGGL(step_kernel, dim3(grid_of(plan->chunks, 65536)), dim3(kThreads), 0, st, a);
+        const dim3 grid(grid_of(plan->chunks, 65536));
+        if (a.eight) hipLaunchKernelGGL(step_kernel<true>, grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL(step_kernel<false>, grid, dim3(kThreads), 0, st, a);
         AW_LAUNCHED();
     }
     hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1), 0, st, a);
