@@ -7,6 +7,7 @@
 #include "profile.h"
 
 #include <algorithm>
+#include <type_traits>
 #include <vector>
 
 namespace gswa {
@@ -17,7 +18,10 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kBlock = 256;             // elements that share an exponent: four for each lane of a wavefront
 constexpr int kChunkBlocks = 8;         // blocks of one piece of work: two for each wavefront of a workgroup
 constexpr long kChunk = (long)kBlock * kChunkBlocks;
-constexpr int kNormBlocks = 1024;
+constexpr int kNormBlocks = 1024;       // workgroups of the norm, at most
+constexpr int kStepBlocks = 4096;       // and of the step: more than run at once
+constexpr int kGroups = 32;             // of the workgroups that are counted together (see last_of_all)
+constexpr int kCounterStep = 32;        // counters stand in lines of their own
 
 // A tensor as the kernels see it.
 struct Tensor {
@@ -33,7 +37,7 @@ struct Tensor {
     int p_bf16, g_bf16;
 };
 
-// The plan's buffer: [Tensor * n][tensor of every piece of work, int][partial sums of the norm][counter]
+// The plan's buffer: [Tensor * n][tensor of every piece of work, int][partial sums of the norm][counters]
 struct Layout {
     size_t owner, part, counter, bytes;
 };
@@ -43,7 +47,7 @@ Layout layout(int n, long chunks)
     l.owner = to_256((size_t)n * sizeof(Tensor));
     l.part = l.owner + to_256((size_t)chunks * sizeof(int));
     l.counter = l.part + to_256(kNormBlocks * sizeof(double));
-    l.bytes = l.counter + 256;
+    l.bytes = l.counter + to_256((kGroups + 1) * kCounterStep * sizeof(unsigned));
     return l;
 }
 
@@ -76,10 +80,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a)
 {
     const Tensor &t = a.t[blockIdx.x];
     const int index = a.first + (int)blockIdx.x;
-    if (threadIdx.x == 0) {
-        a.tensors[index] = t;
-        if (index == 0) *a.counter = 0;
-    }
+    if (threadIdx.x == 0) a.tensors[index] = t;
+    if (index == 0 && threadIdx.x <= kGroups) a.counter[threadIdx.x * kCounterStep] = 0;
     const int chunks = (int)((t.n + kChunk - 1) / kChunk);
     for (int c = threadIdx.x; c < chunks; c += kThreads) a.owner[t.first_chunk + c] = index;
 }
@@ -93,38 +95,58 @@ __device__ __forceinline__ uint32_t mix(uint32_t x)
     return x ^ x >> 16;
 }
 
-// A lane's four elements of a block, from `i` on, as many of them as the tensor has; a whole four by one wide access.
-template <typename T> __device__ __forceinline__ void load4(const T *p, int left, T (&v)[4])
+// Four elements of a lane.  Pointers come out of the plan, so the compiler has to be told that they point at global memory; `base` is the same for a
+// wavefront.  FULL: all four are there, one wide access; else the first `left` of them, zeros for the others.
+template <typename E> using Global = __attribute__((address_space(1))) E;
+template <typename E> struct Four;
+template <> struct Four<float> { typedef u32x4 V; };
+template <> struct Four<bf16_t> { typedef u32x2 V; };
+template <> struct Four<uint8_t> { typedef uint32_t V; };
+template <typename E, bool FULL> __device__ __forceinline__ typename Four<E>::V load4(const void *base, int lane, int left)
 {
-    if (left >= 4) {
-        __builtin_memcpy(v, __builtin_assume_aligned(p, 4 * sizeof(T) < 16 ? 4 * sizeof(T) : 16), 4 * sizeof(T));
+    typedef typename Four<E>::V V;
+    if constexpr (FULL) {
+        return ((const Global<V> *)base)[lane];
     } else {
+        typedef typename std::conditional<sizeof(E) == 1, uint8_t, typename std::conditional<sizeof(E) == 2, uint16_t, uint32_t>::type>::type Bits;
+        Bits e[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = j < left ? p[j] : T{};
+        for (int j = 0; j < 4; ++j) e[j] = j < left ? ((const Global<Bits> *)base)[lane * 4 + j] : Bits(0);
+        V v;
+        __builtin_memcpy(&v, e, sizeof(v));
+        return v;
     }
 }
-template <typename T> __device__ __forceinline__ void store4(T *p, int left, const T (&v)[4])
+template <typename E, bool FULL> __device__ __forceinline__ void store4(void *base, int lane, int left, typename Four<E>::V v)
 {
-    if (left >= 4) {
-        __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(T) < 16 ? 4 * sizeof(T) : 16), v, 4 * sizeof(T));
+    typedef typename Four<E>::V V;
+    if constexpr (FULL) {
+        ((Global<V> *)base)[lane] = v;
     } else {
+        typedef typename std::conditional<sizeof(E) == 1, uint8_t, typename std::conditional<sizeof(E) == 2, uint16_t, uint32_t>::type>::type Bits;
+        Bits e[4];
+        __builtin_memcpy(e, &v, sizeof(v));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (j < left) p[j] = v[j];
+            if (j < left) ((Global<Bits> *)base)[lane * 4 + j] = e[j];
     }
 }
-// (bf16 or fp32 by a flag of the tensor, the same for a whole wavefront)
-__device__ __forceinline__ void load4_as(const void *p, long i, bool bf16, int left, float (&f)[4])
+__device__ __forceinline__ void floats(u32x4 v, float (&f)[4])
 {
-    if (bf16) {
-        bf16_t v[4];
-        load4(static_cast<const bf16_t *>(p) + i, left, v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f[j] = to_f32(v[j]);
-    } else {
-        load4(static_cast<const float *>(p) + i, left, f);
-    }
+    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(v[j]);
 }
+__device__ __forceinline__ void floats(u32x2 v, float (&f)[4])
+{
+    f[0] = bf16_lo(v[0]); f[1] = bf16_hi(v[0]);
+    f[2] = bf16_lo(v[1]); f[3] = bf16_hi(v[1]);
+}
+__device__ __forceinline__ u32x4 patterns(const float (&f)[4])
+{
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+}
+template <typename E> __device__ __forceinline__ const void *at(const void *p, long i) { return static_cast<const char *>(p) + i * (long)sizeof(E); }
+template <typename E> __device__ __forceinline__ void *at(void *p, long i) { return static_cast<char *>(p) + i * (long)sizeof(E); }
 
 // a wavefront's largest pattern
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t v)
@@ -144,26 +166,74 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
     return r[0] > r[1] ? r[0] : r[1];
 }
 
-// Value of code c (without its sign) in a block of exponent E, and the code of a magnitude's pattern rounded by 16 random bits.
-template <int TOP> __device__ __forceinline__ float decode(uint32_t c, int E)
+// Codes of a block.  Its exponent is the same for a wavefront, so what follows from it is kept in scalar registers: `base` is the pattern (upper 12 bits) of code 0.
+template <int TOP> __device__ __forceinline__ int base_of(int E) { return 8 * (E + 1) - TOP; }
+__device__ __forceinline__ uint32_t byte_of(uint32_t word, int j) { return word >> (8 * j) & 255u; }
+
+// the magnitude's pattern that code c stands for (not of a block with E = 255)
+__device__ __forceinline__ uint32_t decode(uint32_t c, int base)
 {
-    const int T = 8 * (E + 1) - TOP + (int)c;
-    const uint32_t bits = c ? (uint32_t)(T > 1 ? T : 1) << 20 : 0u;
-    return __uint_as_float(E == 255 ? 0x7fc00000u : bits);
+    const int T = base + (int)c;
+    return c ? (uint32_t)(T > 1 ? T : 1) << 20 : 0u;
 }
-template <int TOP> __device__ __forceinline__ uint32_t encode(uint32_t bits, int E, uint32_t noise)
+__device__ __forceinline__ void decode_m(uint32_t word, int E, float (&m)[4])
 {
-    constexpr int least = TOP == 255 ? 1 : 0; // (a second moment that is not 0 is not stored as 0)
-    int T = (int)((bits + (noise << 4)) >> 20);
-    const bool none = least ? bits == 0 : T < 1;
-    T = T > 1 ? T : 1;
-    const int c = T - (8 * (E + 1) - TOP), most = E == 254 ? TOP - 1 : TOP;
-    return none || E == 255 ? 0u : (uint32_t)(c < least ? least : c > most ? most : c);
+    const int base = base_of<127>(E);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = __uint_as_float(decode(byte_of(word, j) & 127u, base) | (word << (24 - 8 * j) & 0x80000000u));
+    if (E == 255) m[0] = m[1] = m[2] = m[3] = __uint_as_float(0x7fc00000u);
+}
+__device__ __forceinline__ void decode_v(uint32_t word, int E, float (&v)[4])
+{
+    const int base = base_of<255>(E);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(decode(byte_of(word, j), base));
+    if (E == 255) v[0] = v[1] = v[2] = v[3] = __uint_as_float(0x7fc00000u);
+}
+
+// m's codes, the low 16 bits of h against what is cut off, and v's, the high ones (what is not 0 is not stored as 0)
+__device__ __forceinline__ uint32_t encode_m(const float (&m)[4], int E, const uint32_t (&h)[4])
+{
+    const int base = base_of<127>(E), most = E == 254 ? 126 : 127;
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t bits = __float_as_uint(m[j]);
+        const int T = (int)(((bits & 0x7fffffffu) + ((h[j] & 0xffffu) << 4)) >> 20);
+        int c = T - base;
+        c = c < 0 ? 0 : c > most ? most : c;
+        if (T < 1) c = 0;
+        const uint32_t code = (uint32_t)c | (c ? bits >> 24 & 128u : 0u);
+        word |= code << (8 * j);
+    }
+    return E == 255 ? 0u : word;
+}
+__device__ __forceinline__ uint32_t encode_v(const float (&v)[4], int E, const uint32_t (&h)[4])
+{
+    const int base = base_of<255>(E), most = E == 254 ? 254 : 255;
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t bits = __float_as_uint(v[j]) & 0x7fffffffu;
+        const int T = (int)((bits + ((h[j] >> 16) << 4)) >> 20);
+        int c = (T > 1 ? T : 1) - base;
+        c = c < 1 ? 1 : c > most ? most : c;
+        word |= (bits ? (uint32_t)c : 0u) << (8 * j);
+    }
+    return E == 255 ? 0u : word;
+}
+
+// sqrt to a unit of its last place, of subnormal numbers too (the instruction takes those for 0)
+__device__ __forceinline__ float root_of(float v)
+{
+    const bool small = v < 0x1p-96f;
+    const float s = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
+    return small ? s * 0x1p-32f : s;
 }
 
 // What a step needs of its number and rates, the same for all elements.
 struct Rates {
-    float lr, rate, root, clip; // learning rate; over 1 - beta1^t; sqrt(1 - beta2^t); factor of the gradients
+    float lr, rate, root, clip; // learning rate; over 1 - beta1^t; 1 / sqrt(1 - beta2^t); factor of the gradients
     uint32_t key;
 };
 __device__ __forceinline__ Rates rates_of(const Step &a, float norm)
@@ -178,7 +248,7 @@ __device__ __forceinline__ Rates rates_of(const Step &a, float norm)
     Rates r;
     r.lr = a.lr_scale ? a.lr * *a.lr_scale : a.lr;
     r.rate = r.lr / (float)(1. - b1);
-    r.root = sqrtf((float)(1. - b2));
+    r.root = (float)(1. / sqrt(1. - b2));
     r.clip = a.max_norm > 0.f && norm > a.max_norm ? a.max_norm / norm : 1.f;
     r.key = mix(mix(a.seed_hi ^ 0x510E527Fu) ^ a.seed_lo);
     r.key = mix(mix(r.key ^ (uint32_t)(t >> 32)) ^ (uint32_t)t);
@@ -194,176 +264,256 @@ __device__ __forceinline__ void moments(const Step &a, float g, float &m, float 
     v = v * a.b2 + g * g * a.b2c;
 }
 
-// Bound by memory: 16 to 30 bytes an element against some 40 operations.  A workgroup takes pieces of 8 blocks, a wavefront two of them with all loads of both
-// in flight together; a block's largest magnitude comes from exchanges between its lanes.
+// Whether this workgroup is the last of its launch to come here (one thread of each does, when it needs nothing more that the last one changes).  Arrivals at
+// one address take 15 ns each, whatever they overlap with, so those of a large launch are counted in 32 groups first (a step over 468 tensors, 792 workgroups:
+// 14.8 -> 9.1 us).  Nothing but the count is handed over, so no order of memory is asked for.  Counters are left at 0 for the next launch.
+__device__ __forceinline__ bool arrived_last(unsigned *counter, unsigned all)
+{
+    if (__hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != all - 1) return false;
+    *counter = 0;
+    return true;
+}
+__device__ __forceinline__ bool last_of_all(unsigned *counters)
+{
+    if (gridDim.x <= 2 * kGroups) return arrived_last(counters, gridDim.x);
+    const unsigned group = blockIdx.x % kGroups, members = (gridDim.x - group + kGroups - 1) / kGroups;
+    return arrived_last(counters + (1 + group) * kCounterStep, members) && arrived_last(counters, kGroups);
+}
+
+enum { kP32 = 0, kP16 = 1, kPBoth = 2 }; // the parameter: fp32; bf16; bf16 with an fp32 copy
+
+// N blocks of a tensor in a row; all of their loads first.
+template <int P, typename G, bool EIGHT, int N, bool FULL>
+__device__ __forceinline__ void step_blocks(const Step &a, const Rates &r, const Tensor &T, long first, int lane)
+{
+    typedef typename std::conditional<P == kP16, bf16_t, float>::type Held; // what the parameter is read from
+    typename Four<G>::V g4[N];
+    typename Four<Held>::V p4[N];
+    u32x4 m4[N], v4[N];
+    uint32_t cm[N], cv[N];
+    int em[N], ev[N], left[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const long block = first + k, i = block * kBlock;
+        const long n = T.n - i - lane * 4;
+        left[k] = FULL ? 4 : n < 0 ? 0 : n < 4 ? (int)n : 4;
+        g4[k] = load4<G, FULL>(at<G>(T.g, i), lane, left[k]);
+        p4[k] = load4<Held, FULL>(at<Held>(P == kPBoth ? (const void *)T.master : T.p, i), lane, left[k]);
+        if constexpr (EIGHT) {
+            cm[k] = load4<uint8_t, FULL>(at<uint8_t>(T.m, i), lane, left[k]);
+            cv[k] = load4<uint8_t, FULL>(at<uint8_t>(T.v, i), lane, left[k]);
+            em[k] = ((const Global<uint8_t> *)T.m_exp)[block];
+            ev[k] = ((const Global<uint8_t> *)T.v_exp)[block];
+        } else {
+            m4[k] = load4<float, FULL>(at<float>(T.m, i), lane, left[k]);
+            v4[k] = load4<float, FULL>(at<float>(T.v, i), lane, left[k]);
+        }
+    }
+    const float keep = 1.f - r.lr * T.decay;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const long block = first + k, i = block * kBlock;
+        float g[4], p[4], m[4], v[4];
+        floats(g4[k], g);
+        floats(p4[k], p);
+        if constexpr (EIGHT) {
+            decode_m(cm[k], __builtin_amdgcn_readfirstlane(em[k]), m);
+            decode_v(cv[k], __builtin_amdgcn_readfirstlane(ev[k]), v);
+        } else {
+            floats(m4[k], m);
+            floats(v4[k], v);
+        }
+        uint32_t mmax = 0, vmax = 0; // (elements behind the tensor's end are zeros throughout)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            moments(a, g[j] * r.clip, m[j], v[j]);
+            // (quotient and root to a unit of their last places: the update is some 1e-3 of the parameter)
+            p[j] = p[j] * keep - r.rate * m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * r.root + a.eps);
+            if constexpr (EIGHT) {
+                const uint32_t mb = __float_as_uint(m[j]) & 0x7fffffffu, vb = __float_as_uint(v[j]) & 0x7fffffffu;
+                mmax = mb > mmax ? mb : mmax;
+                vmax = vb > vmax ? vb : vmax;
+            }
+        }
+        uint32_t h[4];
+        if constexpr (EIGHT || P == kP16) {
+            const uint64_t number = (uint64_t)(T.first_block + block) * kBlock; // of the block's first element: no block crosses 2^32
+            const uint32_t key = mix(r.key ^ (uint32_t)(number >> 32)), low = (uint32_t)number + lane * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[j] = mix((low + j) ^ key);
+        }
+        if constexpr (P == kP16) {
+            uint32_t q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { // (an infinity stays one: its 16 bits behind are 0)
+                const uint32_t bits = __float_as_uint(p[j]) + (mix(h[j] ^ 0xBB67AE85u) & 0xffffu);
+                q[j] = p[j] == p[j] ? bits : 0x7fc00000u;
+            }
+            store4<bf16_t, FULL>(at<bf16_t>(T.p, i), lane, left[k], u32x2{q[0] >> 16 | (q[1] & 0xffff0000u), q[2] >> 16 | (q[3] & 0xffff0000u)});
+        } else if constexpr (P == kPBoth) {
+            store4<bf16_t, FULL>(at<bf16_t>(T.p, i), lane, left[k], u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])});
+            store4<float, FULL>(at<float>((void *)T.master, i), lane, left[k], patterns(p));
+        } else {
+            store4<float, FULL>(at<float>(T.p, i), lane, left[k], patterns(p));
+        }
+        if constexpr (EIGHT) {
+            const int Em = __builtin_amdgcn_readfirstlane(wave_max(mmax) >> 23), Ev = __builtin_amdgcn_readfirstlane(wave_max(vmax) >> 23);
+            if (lane == 0) {
+                ((Global<uint8_t> *)T.m_exp)[block] = (uint8_t)Em;
+                ((Global<uint8_t> *)T.v_exp)[block] = (uint8_t)Ev;
+            }
+            store4<uint8_t, FULL>(at<uint8_t>(T.m, i), lane, left[k], encode_m(m, Em, h));
+            store4<uint8_t, FULL>(at<uint8_t>(T.v, i), lane, left[k], encode_v(v, Ev, h));
+        } else {
+            store4<float, FULL>(at<float>(T.m, i), lane, left[k], patterns(m));
+            store4<float, FULL>(at<float>(T.v, i), lane, left[k], patterns(v));
+        }
+    }
+}
+
+// The two blocks of a piece of work that a wavefront takes: both at once where they are whole, one by one at a tensor's end.
+template <typename F, typename H> __device__ __forceinline__ void each_block(const Tensor &T, long chunk, int wave, F whole, H partly)
+{
+    static_assert(kChunkBlocks == 2 * kWaves, "two blocks a wavefront");
+    const long first = (chunk - T.first_chunk) * kChunkBlocks + 2 * wave;
+    if ((first + 2) * kBlock <= T.n) return whole(first);
+    for (long b = first; b < first + 2; ++b)
+        if (b * kBlock < T.n) partly(b);
+}
+
+// Bound by memory: 16 to 30 bytes an element against about a hundred operations with 8-bit states, half of that with 32.  A workgroup takes pieces of 8 blocks, a
+// wavefront two of them with all loads of both in flight together; a block's largest magnitude comes from exchanges between its lanes.
 template <bool EIGHT> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
 {
-    constexpr int kEach = kChunkBlocks / kWaves;
     const float norm = a.norm ? *a.norm : 0.f;
     if (a.skip && !(fabsf(norm) < INFINITY)) return;
     const Rates r = rates_of(a, norm);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Tensor T = a.tensors[a.owner[chunk]];
-        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
-        float g[kEach][4], p[kEach][4], m[kEach][4], v[kEach][4];
-        uint8_t cm[kEach][4], cv[kEach][4];
-        int em[kEach], ev[kEach], left[kEach];
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const long block = first + k * kWaves, i = block * kBlock + lane * 4, n = T.n - i;
-            left[k] = n < 0 ? 0 : n < 4 ? (int)n : 4;
-            if (block * kBlock >= T.n) continue;
-            load4_as(T.g, i, T.g_bf16, left[k], g[k]);
-            if (T.master) load4(T.master + i, left[k], p[k]);
-            else load4_as(T.p, i, T.p_bf16, left[k], p[k]);
-            if (EIGHT) {
-                load4(static_cast<const uint8_t *>(T.m) + i, left[k], cm[k]);
-                load4(static_cast<const uint8_t *>(T.v) + i, left[k], cv[k]);
-                em[k] = T.m_exp[block];
-                ev[k] = T.v_exp[block];
-            } else {
-                load4(static_cast<const float *>(T.m) + i, left[k], m[k]);
-                load4(static_cast<const float *>(T.v) + i, left[k], v[k]);
-            }
-        }
-        const float keep = 1.f - r.lr * T.decay;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const long block = first + k * kWaves, i = block * kBlock + lane * 4;
-            if (block * kBlock >= T.n) continue;
-            uint32_t mmax = 0, vmax = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (EIGHT) {
-                    m[k][j] = decode<127>(cm[k][j] & 127, em[k]);
-                    if (cm[k][j] & 128) m[k][j] = -m[k][j];
-                    v[k][j] = decode<255>(cv[k][j], ev[k]);
-                }
-                moments(a, g[k][j] * r.clip, m[k][j], v[k][j]);
-                p[k][j] = p[k][j] * keep - r.rate * m[k][j] / (sqrtf(v[k][j]) / r.root + a.eps);
-                if (EIGHT && j < left[k]) {
-                    const uint32_t mb = __float_as_uint(m[k][j]) & 0x7fffffffu, vb = __float_as_uint(v[k][j]) & 0x7fffffffu;
-                    mmax = mb > mmax ? mb : mmax;
-                    vmax = vb > vmax ? vb : vmax;
-                }
-            }
-            const uint64_t number = (uint64_t)(T.first_block + block) * kBlock + lane * 4;
-            uint32_t h[4];
-            const bool noisy = T.p_bf16 && !T.master;
-            if (EIGHT || noisy) {
-                const uint32_t key = mix(r.key ^ (uint32_t)(number >> 32));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = mix(((uint32_t)number + j) ^ key);
-            }
-            if (T.p_bf16) {
-                bf16_t q[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (noisy) {
-                        uint32_t bits = __float_as_uint(p[k][j]);
-                        if ((bits & 0x7f800000u) != 0x7f800000u) bits += mix(h[j] ^ 0xBB67AE85u) & 0xffffu;
-                        q[j].bits = p[k][j] == p[k][j] ? (uint16_t)(bits >> 16) : (uint16_t)0x7fc0;
-                    } else {
-                        from_f32(q[j], p[k][j]);
-                    }
-                }
-                store4(static_cast<bf16_t *>(T.p) + i, left[k], q);
-                if (T.master) store4(T.master + i, left[k], p[k]);
-            } else {
-                store4(static_cast<float *>(T.p) + i, left[k], p[k]);
-            }
-            if (EIGHT) {
-                const int Em = (int)(wave_max(mmax) >> 23), Ev = (int)(wave_max(vmax) >> 23);
-                if (lane == 0) {
-                    T.m_exp[block] = (uint8_t)Em;
-                    T.v_exp[block] = (uint8_t)Ev;
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t mb = __float_as_uint(m[k][j]);
-                    const uint32_t c = encode<127>(mb & 0x7fffffffu, Em, h[j] & 0xffffu);
-                    cm[k][j] = (uint8_t)(c | (c ? mb >> 24 & 128u : 0u));
-                    cv[k][j] = (uint8_t)encode<255>(__float_as_uint(v[k][j]) & 0x7fffffffu, Ev, h[j] >> 16);
-                }
-                store4(static_cast<uint8_t *>(T.m) + i, left[k], cm[k]);
-                store4(static_cast<uint8_t *>(T.v) + i, left[k], cv[k]);
-            } else {
-                store4(static_cast<float *>(T.m) + i, left[k], m[k]);
-                store4(static_cast<float *>(T.v) + i, left[k], v[k]);
-            }
-        }
+        const auto go = [&](auto p, auto g) {
+            typedef decltype(g) G;
+            constexpr int P = decltype(p)::value;
+            each_block(T, chunk, wave, [&](long b) { step_blocks<P, G, EIGHT, 2, true>(a, r, T, b, lane); },
+                       [&](long b) { step_blocks<P, G, EIGHT, 1, false>(a, r, T, b, lane); });
+        };
+        const auto by_gradient = [&](auto p) {
+            if (T.g_bf16) go(p, bf16_t{});
+            else go(p, float{});
+        };
+        if (!T.p_bf16) by_gradient(std::integral_constant<int, kP32>{});
+        else if (T.master) by_gradient(std::integral_constant<int, kPBoth>{});
+        else by_gradient(std::integral_constant<int, kP16>{});
     }
+    // (every workgroup has read the number of steps before)
+    if (threadIdx.x == 0 && last_of_all(a.counter)) *a.step += 1;
 }
 
-// behind the step, on the same stream
-__global__ void count_kernel(Step a)
+__device__ __forceinline__ double block_sum(double v)
 {
-    if (a.skip && !(fabsf(*a.norm) < INFINITY)) return;
-    *a.step += 1;
+    __shared__ double lds[kWaves];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// Squares are summed in fp64, which costs nothing beside the reads: no gradient's square overflows or is lost.
+// Four squares are added in fp32 and go on in fp64, so no sum over many elements loses digits; where a square could overflow or be lost (the sum of four
+// is out of bounds or hardly above 0) they are formed in fp64 too.  A launch of its own adds up what the workgroups leave, in their order: in one launch, with the
+// last workgroup adding, each of them has to write its caches back first, and 792 of them took 16 us where the two launches take 10.
 __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
 {
-    constexpr int kEach = kChunkBlocks / kWaves;
-    __shared__ double lds[kWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     double s = 0.;
+    const auto add = [&](const float (&g)[4]) {
+        const float q = (g[0] * g[0] + g[1] * g[1]) + (g[2] * g[2] + g[3] * g[3]);
+        if (q > 1e-30f && q < 3e38f) {
+            s += (double)q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += (double)g[j] * (double)g[j];
+        }
+    };
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Tensor T = a.tensors[a.owner[chunk]];
-        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
-        float g[kEach][4];
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const long i = (first + k * kWaves) * kBlock + lane * 4, n = T.n - i;
-            load4_as(T.g, i, T.g_bf16, n < 0 ? 0 : n < 4 ? (int)n : 4, g[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kEach; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s += (double)g[k][j] * (double)g[k][j];
+        const auto go = [&](auto g) {
+            typedef decltype(g) G;
+            each_block(T, chunk, wave,
+                       [&](long b) {
+                           float f[4], h[4];
+                           const auto x = load4<G, true>(at<G>(T.g, b * kBlock), lane, 4), y = load4<G, true>(at<G>(T.g, (b + 1) * kBlock), lane, 4);
+                           floats(x, f);
+                           floats(y, h);
+                           add(f);
+                           add(h);
+                       },
+                       [&](long b) {
+                           const long n = T.n - b * kBlock - lane * 4;
+                           float f[4];
+                           floats(load4<G, false>(at<G>(T.g, b * kBlock), lane, n < 0 ? 0 : n < 4 ? (int)n : 4), f);
+                           add(f);
+                       });
+        };
+        if (T.g_bf16) go(bf16_t{});
+        else go(float{});
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) lds[wave] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) a.part[blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    s = block_sum(s);
+    if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(64) void norm_sum_kernel(Step a, int parts)
+__global__ __launch_bounds__(kThreads) void norm_sum_kernel(Step a, int parts)
 {
     double s = 0.;
-    for (int i = threadIdx.x; i < parts; i += 64) s += a.part[i];
-#pragma unroll
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    for (int i = threadIdx.x; i < parts; i += kThreads) s += a.part[i];
+    s = block_sum(s);
     if (threadIdx.x == 0) *a.norm_out = (float)sqrt(s);
+}
+
+// Two whole blocks, eight codes a lane: half a wavefront a block.
+template <typename Decode> __device__ __forceinline__ void unpack_whole(const void *codes, const uint8_t *exp, uint16_t *out, long block, int lane, Decode decode)
+{
+    const u32x2 c = ((const Global<u32x2> *)at<uint8_t>(codes, block * kBlock))[lane];
+    const int E = ((const Global<uint8_t> *)exp)[block + lane / 32];
+    float f[8];
+    decode(c[0], E, reinterpret_cast<float (&)[4]>(f[0]));
+    decode(c[1], E, reinterpret_cast<float (&)[4]>(f[4]));
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(f[2 * j]) >> 16 | (__float_as_uint(f[2 * j + 1]) & 0xffff0000u);
+    ((Global<u32x4> *)out)[lane] = w;
+}
+// The block at a tensor's end, zeros behind it.
+template <typename Decode> __device__ __forceinline__ void unpack_end(const void *codes, const uint8_t *exp, uint16_t *out, long block, long n, int lane, Decode decode)
+{
+    const long over = n - block * kBlock - lane * 4;
+    const int left = over < 0 ? 0 : over < 4 ? (int)over : 4;
+    float f[4];
+    decode(load4<uint8_t, false>(at<uint8_t>(codes, block * kBlock), lane, left), ((const Global<uint8_t> *)exp)[block], f);
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = j < left ? __float_as_uint(f[j]) : 0u;
+    ((Global<u32x2> *)out)[lane] = u32x2{u[0] >> 16 | (u[1] & 0xffff0000u), u[2] >> 16 | (u[3] & 0xffff0000u)};
 }
 
 __global__ __launch_bounds__(kThreads) void unpack_kernel(Step a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const auto of_m = [](uint32_t word, int E, float (&f)[4]) { decode_m(word, E, f); };
+    const auto of_v = [](uint32_t word, int E, float (&f)[4]) { decode_v(word, E, f); };
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Tensor T = a.tensors[a.owner[chunk]];
-        const long first = (chunk - T.first_chunk) * kChunkBlocks + wave;
-#pragma unroll
-        for (int k = 0; k < kChunkBlocks / kWaves; ++k) {
-            const long block = first + k * kWaves, i = block * kBlock + lane * 4, n = T.n - i, at = T.first_block * kBlock + i;
-            if (block * kBlock >= T.n) break;
-            const int left = n < 0 ? 0 : n < 4 ? (int)n : 4;
-            uint8_t cm[4] = {}, cv[4] = {};
-            if (a.m_out) load4(static_cast<const uint8_t *>(T.m) + i, left, cm);
-            if (a.v_out) load4(static_cast<const uint8_t *>(T.v) + i, left, cv);
-            const int em = T.m_exp[block], ev = T.v_exp[block];
-            uint16_t m[4], v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { // (zeros behind the tensor's end)
-                m[j] = j < left ? (uint16_t)(__float_as_uint(decode<127>(cm[j] & 127, em)) >> 16 | (cm[j] & 128) << 8) : 0;
-                v[j] = j < left ? (uint16_t)(__float_as_uint(decode<255>(cv[j], ev)) >> 16) : 0;
-            }
-            if (a.m_out) store4(a.m_out + at, 4, m);
-            if (a.v_out) store4(a.v_out + at, 4, v);
-        }
+        each_block(T, chunk, wave,
+                   [&](long b) {
+                       const long to = (T.first_block + b) * kBlock;
+                       if (a.m_out) unpack_whole(T.m, T.m_exp, a.m_out + to, b, lane, of_m);
+                       if (a.v_out) unpack_whole(T.v, T.v_exp, a.v_out + to, b, lane, of_v);
+                   },
+                   [&](long b) {
+                       const long to = (T.first_block + b) * kBlock;
+                       if (a.m_out) unpack_end(T.m, T.m_exp, a.m_out + to, b, T.n, lane, of_m);
+                       if (a.v_out) unpack_end(T.v, T.v_exp, a.v_out + to, b, T.n, lane, of_v);
+                   });
     }
 }
 
@@ -454,7 +604,7 @@ int check_ranges(const adamw_desc *d, const adamw_tensor *t, int n, const void *
     return GSWA_OK;
 }
 
-unsigned grid_of(long chunks, long most) { return (unsigned)(chunks < most ? chunks : most); }
+unsigned grid_of(long chunks, long most) { return (unsigned)(chunks < 1 ? 1 : chunks < most ? chunks : most); }
 
 } // namespace
 } // namespace gswa
@@ -533,13 +683,11 @@ int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream)
     fill(plan, &a);
     a.norm_out = norm;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned grid = grid_of(plan->chunks, kNormBlocks);
     KernelTimer t(K_ADAMW_NORM, st);
-    if (grid) {
-        hipLaunchKernelGGL(norm_kernel, dim3(grid), dim3(kThreads), 0, st, a);
-        AW_LAUNCHED();
-    }
-    hipLaunchKernelGGL(norm_sum_kernel, dim3(1), dim3(64), 0, st, a, (int)grid);
+    const unsigned grid = grid_of(plan->chunks, kNormBlocks);
+    hipLaunchKernelGGL(norm_kernel, dim3(grid), dim3(kThreads), 0, st, a);
+    AW_LAUNCHED();
+    hipLaunchKernelGGL(norm_sum_kernel, dim3(1), dim3(kThreads), 0, st, a, (int)grid);
     AW_LAUNCHED();
     return GSWA_OK;
 }
@@ -555,13 +703,9 @@ int adamw_step(const adamw_plan_t *plan, int64_t *step, float lr, const float *l
     a.step = step; a.lr = lr; a.lr_scale = lr_scale; a.norm = norm; a.max_norm = max_norm;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_STEP, st);
-    if (plan->chunks) {
-        const dim3 grid(grid_of(plan->chunks, 65536));
-        if (a.eight) hipLaunchKernelGGL(step_kernel<true>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(step_kernel<false>, grid, dim3(kThreads), 0, st, a);
-        AW_LAUNCHED();
-    }
-    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1), 0, st, a);
+    const dim3 grid(grid_of(plan->chunks, kStepBlocks));
+    if (a.eight) hipLaunchKernelGGL(step_kernel<true>, grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(step_kernel<false>, grid, dim3(kThreads), 0, st, a);
     AW_LAUNCHED();
     return GSWA_OK;
 }
@@ -580,7 +724,7 @@ int adamw_unpack(const adamw_plan_t *plan, void *m_out, void *v_out, void *hip_s
     a.v_out = static_cast<uint16_t *>(v_out);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_UNPACK, st);
-    hipLaunchKernelGGL(unpack_kernel, dim3(grid_of(plan->chunks, 65536)), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(unpack_kernel, dim3(grid_of(plan->chunks, kStepBlocks)), dim3(kThreads), 0, st, a);
     AW_LAUNCHED();
     return GSWA_OK;
 }
