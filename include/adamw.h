@@ -73,7 +73,7 @@ typedef struct adamw_tensor {
  */
 typedef struct adamw_plan_t {
     adamw_desc desc;
-    int32_t n_tensors;
+    int32_t n_tensors, each;
     int64_t chunks;   /* pieces of work                                                                   */
     int64_t blocks;   /* blocks of 256 elements                                                           */
     void *buffer;

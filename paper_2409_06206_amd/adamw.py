@@ -27,7 +27,7 @@ class adamw_tensor(ctypes.Structure):
 
 
 class adamw_plan_t(ctypes.Structure):
-    _fields_ = [("desc", adamw_desc), ("n_tensors", ctypes.c_int32), ("chunks", ctypes.c_int64), ("blocks", ctypes.c_int64),
+    _fields_ = [("desc", adamw_desc), ("n_tensors", ctypes.c_int32), ("each", ctypes.c_int32), ("chunks", ctypes.c_int64), ("blocks", ctypes.c_int64),
                 ("buffer", ctypes.c_void_p), ("check", ctypes.c_uint64)]
 
 

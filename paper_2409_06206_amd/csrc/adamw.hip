@@ -16,12 +16,17 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBlock = 256;             // elements that share an exponent: four for each lane of a wavefront
-constexpr int kChunkBlocks = 8;         // blocks of one piece of work: two for each wavefront of a workgroup
-constexpr long kChunk = (long)kBlock * kChunkBlocks;
 constexpr int kNormBlocks = 1024;       // workgroups of the norm, at most
-constexpr int kStepBlocks = 4096;       // and of the step: more than run at once
+constexpr int kStepBlocks = 65536;      // and of the others: a workgroup a piece of work up to 268 M elements (201 M, fp32: 1042 us; 4096 workgroups that
+                                        // go on to further pieces 1127 us, 16384 1082 us)
 constexpr int kGroups = 32;             // of the workgroups that are counted together (see last_of_all)
 constexpr int kCounterStep = 32;        // counters stand in lines of their own
+
+// Blocks of a piece of work that a wavefront takes at once: four for large lists, whose loads then keep the memory busy (read-back of 201 M elements: 234 us, with two
+// 308), one for small ones, where a wavefront's time counts (0.9 M elements in 468 tensors, 8-bit states: see kSmall).
+constexpr int kMany = 4;
+constexpr long kSmall = 8192;           // blocks of a list that is small: up to 2 M elements, 8 workgroups a compute unit
+constexpr long chunk_of(int each) { return (long)kBlock * kWaves * each; }
 
 // A tensor as the kernels see it.
 struct Tensor {
@@ -73,7 +78,7 @@ struct PlanArgs {
     Tensor *tensors;
     int *owner;
     unsigned *counter;
-    int first;
+    int first, each;
 };
 
 __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a)
@@ -82,7 +87,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a)
     const int index = a.first + (int)blockIdx.x;
     if (threadIdx.x == 0) a.tensors[index] = t;
     if (index == 0 && threadIdx.x <= kGroups) a.counter[threadIdx.x * kCounterStep] = 0;
-    const int chunks = (int)((t.n + kChunk - 1) / kChunk);
+    const long chunk = chunk_of(a.each);
+    const int chunks = (int)((t.n + chunk - 1) / chunk);
     for (int c = threadIdx.x; c < chunks; c += kThreads) a.owner[t.first_chunk + c] = index;
 }
 
@@ -371,19 +377,18 @@ __device__ __forceinline__ void step_blocks(const Step &a, const Rates &r, const
     }
 }
 
-// The two blocks of a piece of work that a wavefront takes: both at once where they are whole, one by one at a tensor's end.
-template <typename F, typename H> __device__ __forceinline__ void each_block(const Tensor &T, long chunk, int wave, F whole, H partly)
+// The N blocks of a piece of work that a wavefront takes: all at once where they are whole, one by one at a tensor's end.
+template <int N, typename F, typename H> __device__ __forceinline__ void each_block(const Tensor &T, long chunk, int wave, F whole, H partly)
 {
-    static_assert(kChunkBlocks == 2 * kWaves, "two blocks a wavefront");
-    const long first = (chunk - T.first_chunk) * kChunkBlocks + 2 * wave;
-    if ((first + 2) * kBlock <= T.n) return whole(first);
-    for (long b = first; b < first + 2; ++b)
+    const long first = ((chunk - T.first_chunk) * kWaves + wave) * N;
+    if ((first + N) * kBlock <= T.n) return whole(first);
+    for (long b = first; b < first + N; ++b)
         if (b * kBlock < T.n) partly(b);
 }
 
-// Bound by memory: 16 to 30 bytes an element against about a hundred operations with 8-bit states, half of that with 32.  A workgroup takes pieces of 8 blocks, a
-// wavefront two of them with all loads of both in flight together; a block's largest magnitude comes from exchanges between its lanes.
-template <bool EIGHT> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
+// Bound by memory: 16 to 30 bytes an element against about a hundred operations with 8-bit states, half of that with 32.  A wavefront has all loads of
+// N blocks in flight together; a block's largest magnitude comes from exchanges between its lanes.
+template <bool EIGHT, int N> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
 {
     const float norm = a.norm ? *a.norm : 0.f;
     if (a.skip && !(fabsf(norm) < INFINITY)) return;
@@ -394,8 +399,8 @@ template <bool EIGHT> __global__ __launch_bounds__(kThreads) void step_kernel(St
         const auto go = [&](auto p, auto g) {
             typedef decltype(g) G;
             constexpr int P = decltype(p)::value;
-            each_block(T, chunk, wave, [&](long b) { step_blocks<P, G, EIGHT, 2, true>(a, r, T, b, lane); },
-                       [&](long b) { step_blocks<P, G, EIGHT, 1, false>(a, r, T, b, lane); });
+            each_block<N>(T, chunk, wave, [&](long b) { step_blocks<P, G, EIGHT, N, true>(a, r, T, b, lane); },
+                          [&](long b) { step_blocks<P, G, EIGHT, 1, false>(a, r, T, b, lane); });
         };
         const auto by_gradient = [&](auto p) {
             if (T.g_bf16) go(p, bf16_t{});
@@ -422,7 +427,7 @@ __device__ __forceinline__ double block_sum(double v)
 // Four squares are added in fp32 and go on in fp64, so no sum over many elements loses digits; where a square could overflow or be lost (the sum of four
 // is out of bounds or hardly above 0) they are formed in fp64 too.  A launch of its own adds up what the workgroups leave, in their order: in one launch, with the
 // last workgroup adding, each of them has to write its caches back first, and 792 of them took 16 us where the two launches take 10.
-__global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
+template <int N> __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     double s = 0.;
@@ -439,21 +444,24 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
         const Tensor T = a.tensors[a.owner[chunk]];
         const auto go = [&](auto g) {
             typedef decltype(g) G;
-            each_block(T, chunk, wave,
-                       [&](long b) {
-                           float f[4], h[4];
-                           const auto x = load4<G, true>(at<G>(T.g, b * kBlock), lane, 4), y = load4<G, true>(at<G>(T.g, (b + 1) * kBlock), lane, 4);
-                           floats(x, f);
-                           floats(y, h);
-                           add(f);
-                           add(h);
-                       },
-                       [&](long b) {
-                           const long n = T.n - b * kBlock - lane * 4;
-                           float f[4];
-                           floats(load4<G, false>(at<G>(T.g, b * kBlock), lane, n < 0 ? 0 : n < 4 ? (int)n : 4), f);
-                           add(f);
-                       });
+            each_block<N>(T, chunk, wave,
+                          [&](long b) {
+                              typename Four<G>::V v[N];
+#pragma unroll
+                              for (int k = 0; k < N; ++k) v[k] = load4<G, true>(at<G>(T.g, (b + k) * kBlock), lane, 4);
+#pragma unroll
+                              for (int k = 0; k < N; ++k) {
+                                  float f[4];
+                                  floats(v[k], f);
+                                  add(f);
+                              }
+                          },
+                          [&](long b) {
+                              const long n = T.n - b * kBlock - lane * 4;
+                              float f[4];
+                              floats(load4<G, false>(at<G>(T.g, b * kBlock), lane, n < 0 ? 0 : n < 4 ? (int)n : 4), f);
+                              add(f);
+                          });
         };
         if (T.g_bf16) go(bf16_t{});
         else go(float{});
@@ -470,18 +478,33 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(Step a, int parts)
     if (threadIdx.x == 0) *a.norm_out = (float)sqrt(s);
 }
 
-// Two whole blocks, eight codes a lane: half a wavefront a block.
-template <typename Decode> __device__ __forceinline__ void unpack_whole(const void *codes, const uint8_t *exp, uint16_t *out, long block, int lane, Decode decode)
+// N whole blocks: two at a time, eight codes a lane, half a wavefront a block (a single one with four a lane).
+template <int N, typename Decode>
+__device__ __forceinline__ void unpack_whole(const void *codes, const uint8_t *exp, uint16_t *out, long block, int lane, Decode decode)
 {
-    const u32x2 c = ((const Global<u32x2> *)at<uint8_t>(codes, block * kBlock))[lane];
-    const int E = ((const Global<uint8_t> *)exp)[block + lane / 32];
-    float f[8];
-    decode(c[0], E, reinterpret_cast<float (&)[4]>(f[0]));
-    decode(c[1], E, reinterpret_cast<float (&)[4]>(f[4]));
-    u32x4 w;
+    if constexpr (N == 1) {
+        float f[4];
+        decode(((const Global<uint32_t> *)at<uint8_t>(codes, block * kBlock))[lane], ((const Global<uint8_t> *)exp)[block], f);
+        ((Global<u32x2> *)out)[lane] = u32x2{__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
+                                             __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xffff0000u)};
+    } else {
+        u32x2 c[N / 2];
+        int E[N / 2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(f[2 * j]) >> 16 | (__float_as_uint(f[2 * j + 1]) & 0xffff0000u);
-    ((Global<u32x4> *)out)[lane] = w;
+        for (int k = 0; k < N / 2; ++k) {
+            c[k] = ((const Global<u32x2> *)at<uint8_t>(codes, (block + 2 * k) * kBlock))[lane];
+            E[k] = ((const Global<uint8_t> *)exp)[block + 2 * k + lane / 32];
+        }
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) {
+            float lo[4], hi[4];
+            decode(c[k][0], E[k], lo);
+            decode(c[k][1], E[k], hi);
+            const u32x4 w = {__float_as_uint(lo[0]) >> 16 | (__float_as_uint(lo[1]) & 0xffff0000u), __float_as_uint(lo[2]) >> 16 | (__float_as_uint(lo[3]) & 0xffff0000u),
+                             __float_as_uint(hi[0]) >> 16 | (__float_as_uint(hi[1]) & 0xffff0000u), __float_as_uint(hi[2]) >> 16 | (__float_as_uint(hi[3]) & 0xffff0000u)};
+            ((Global<u32x4> *)at<uint16_t>((void *)out, 2 * k * kBlock))[lane] = w;
+        }
+    }
 }
 // The block at a tensor's end, zeros behind it.
 template <typename Decode> __device__ __forceinline__ void unpack_end(const void *codes, const uint8_t *exp, uint16_t *out, long block, long n, int lane, Decode decode)
@@ -496,18 +519,18 @@ template <typename Decode> __device__ __forceinline__ void unpack_end(const void
     ((Global<u32x2> *)out)[lane] = u32x2{u[0] >> 16 | (u[1] & 0xffff0000u), u[2] >> 16 | (u[3] & 0xffff0000u)};
 }
 
-__global__ __launch_bounds__(kThreads) void unpack_kernel(Step a)
+template <int N> __global__ __launch_bounds__(kThreads) void unpack_kernel(Step a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const auto of_m = [](uint32_t word, int E, float (&f)[4]) { decode_m(word, E, f); };
     const auto of_v = [](uint32_t word, int E, float (&f)[4]) { decode_v(word, E, f); };
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Tensor T = a.tensors[a.owner[chunk]];
-        each_block(T, chunk, wave,
+        each_block<N>(T, chunk, wave,
                    [&](long b) {
                        const long to = (T.first_block + b) * kBlock;
-                       if (a.m_out) unpack_whole(T.m, T.m_exp, a.m_out + to, b, lane, of_m);
-                       if (a.v_out) unpack_whole(T.v, T.v_exp, a.v_out + to, b, lane, of_v);
+                       if (a.m_out) unpack_whole<N>(T.m, T.m_exp, a.m_out + to, b, lane, of_m);
+                       if (a.v_out) unpack_whole<N>(T.v, T.v_exp, a.v_out + to, b, lane, of_v);
                    },
                    [&](long b) {
                        const long to = (T.first_block + b) * kBlock;
@@ -524,24 +547,25 @@ bool desc_ok(const adamw_desc *d)
 }
 
 // What the host knows of the list: places among all blocks and pieces of work.
-int count(const adamw_desc *d, const adamw_tensor *t, int n, long *chunks, long *blocks)
+int count(const adamw_desc *d, const adamw_tensor *t, int n, int *each, long *chunks, long *blocks)
 {
     if (!desc_ok(d) || !t || n <= 0) return GSWA_EINVAL;
     *chunks = *blocks = 0;
     for (int i = 0; i < n; ++i) {
         if (t[i].n < 0) return GSWA_EINVAL;
         if (t[i].n > 1L << 40) return GSWA_EUNSUPPORTED;
-        *chunks += (t[i].n + kChunk - 1) / kChunk;
         *blocks += (t[i].n + kBlock - 1) / kBlock;
-        if (*chunks > 0x7fffffffL) return GSWA_EUNSUPPORTED;
+        if (*blocks > 1L << 32) return GSWA_EUNSUPPORTED; // (2^40 elements)
     }
-    return GSWA_OK;
+    *each = *blocks <= kSmall ? 1 : kMany;
+    for (int i = 0; i < n; ++i) *chunks += (t[i].n + chunk_of(*each) - 1) / chunk_of(*each);
+    return *chunks > 0x7fffffffL ? GSWA_EUNSUPPORTED : GSWA_OK;
 }
 
 uint64_t checksum(const adamw_plan_t *p)
 {
     uint64_t h = 0x41646157u;
-    for (uint64_t x : {(uint64_t)p->n_tensors, (uint64_t)p->chunks, (uint64_t)p->blocks, (uint64_t)reinterpret_cast<uintptr_t>(p->buffer),
+    for (uint64_t x : {(uint64_t)p->n_tensors, (uint64_t)p->each, (uint64_t)p->chunks, (uint64_t)p->blocks, (uint64_t)reinterpret_cast<uintptr_t>(p->buffer),
                        (uint64_t)p->desc.state_bits, (uint64_t)p->desc.flags, p->desc.seed})
         h = (h ^ x) * 0x9E3779B97F4A7C15u, h ^= h >> 29;
     return h;
@@ -621,8 +645,9 @@ extern "C" {
 
 int adamw_query_bytes(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_tensors, size_t *plan_bytes)
 {
+    int each;
     long chunks, blocks;
-    const int rc = count(desc, tensors, n_tensors, &chunks, &blocks);
+    const int rc = count(desc, tensors, n_tensors, &each, &chunks, &blocks);
     if (rc != GSWA_OK) return rc;
     if (plan_bytes) *plan_bytes = layout(n_tensors, chunks).bytes;
     return GSWA_OK;
@@ -631,8 +656,9 @@ int adamw_query_bytes(const adamw_desc *desc, const adamw_tensor *tensors, int32
 int adamw_plan(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_tensors, void *buffer, adamw_plan_t *plan,
                void *hip_stream)
 {
+    int each;
     long chunks, blocks;
-    int rc = count(desc, tensors, n_tensors, &chunks, &blocks);
+    int rc = count(desc, tensors, n_tensors, &each, &chunks, &blocks);
     if (rc != GSWA_OK) return rc;
     if (!buffer || !plan || !aligned_to(256, buffer)) return GSWA_EINVAL;
     const bool eight = desc->state_bits == 8;
@@ -649,13 +675,14 @@ int adamw_plan(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_te
     if (rc != GSWA_OK) return rc;
     *plan = adamw_plan_t{};
     plan->desc = *desc;
-    plan->n_tensors = n_tensors; plan->chunks = chunks; plan->blocks = blocks; plan->buffer = buffer;
+    plan->n_tensors = n_tensors; plan->each = each; plan->chunks = chunks; plan->blocks = blocks; plan->buffer = buffer;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     char *b = static_cast<char *>(buffer);
     PlanArgs a;
     a.tensors = reinterpret_cast<Tensor *>(b);
     a.owner = reinterpret_cast<int *>(b + l.owner);
     a.counter = reinterpret_cast<unsigned *>(b + l.counter);
+    a.each = each;
     long block = 0;
     int chunk = 0;
     for (int first = 0; first < n_tensors; first += kPerLaunch) {
@@ -666,7 +693,7 @@ int adamw_plan(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_te
             a.t[i] = Tensor{t.p, t.master, t.g, t.m, t.v, t.m_exp, t.v_exp, t.n, block, chunk, t.weight_decay,
                             t.p_dtype == GSWA_BF16, t.g_dtype == GSWA_BF16};
             block += (t.n + kBlock - 1) / kBlock;
-            chunk += (int)((t.n + kChunk - 1) / kChunk);
+            chunk += (int)((t.n + chunk_of(each) - 1) / chunk_of(each));
         }
         KernelTimer timer(K_ADAMW_PLAN, st);
         hipLaunchKernelGGL(plan_kernel, dim3(now), dim3(kThreads), 0, st, a);
@@ -685,7 +712,8 @@ int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream)
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_NORM, st);
     const unsigned grid = grid_of(plan->chunks, kNormBlocks);
-    hipLaunchKernelGGL(norm_kernel, dim3(grid), dim3(kThreads), 0, st, a);
+    if (plan->each == 1) hipLaunchKernelGGL(norm_kernel<1>, dim3(grid), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(norm_kernel<kMany>, dim3(grid), dim3(kThreads), 0, st, a);
     AW_LAUNCHED();
     hipLaunchKernelGGL(norm_sum_kernel, dim3(1), dim3(kThreads), 0, st, a, (int)grid);
     AW_LAUNCHED();
@@ -704,8 +732,13 @@ int adamw_step(const adamw_plan_t *plan, int64_t *step, float lr, const float *l
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_STEP, st);
     const dim3 grid(grid_of(plan->chunks, kStepBlocks));
-    if (a.eight) hipLaunchKernelGGL(step_kernel<true>, grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(step_kernel<false>, grid, dim3(kThreads), 0, st, a);
+    if (plan->each == 1) {
+        if (a.eight) hipLaunchKernelGGL((step_kernel<true, 1>), grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((step_kernel<false, 1>), grid, dim3(kThreads), 0, st, a);
+    } else {
+        if (a.eight) hipLaunchKernelGGL((step_kernel<true, kMany>), grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL((step_kernel<false, kMany>), grid, dim3(kThreads), 0, st, a);
+    }
     AW_LAUNCHED();
     return GSWA_OK;
 }
@@ -724,7 +757,9 @@ int adamw_unpack(const adamw_plan_t *plan, void *m_out, void *v_out, void *hip_s
     a.v_out = static_cast<uint16_t *>(v_out);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     KernelTimer t(K_ADAMW_UNPACK, st);
-    hipLaunchKernelGGL(unpack_kernel, dim3(grid_of(plan->chunks, kStepBlocks)), dim3(kThreads), 0, st, a);
+    const dim3 grid(grid_of(plan->chunks, kStepBlocks));
+    if (plan->each == 1) hipLaunchKernelGGL(unpack_kernel<1>, grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(unpack_kernel<kMany>, grid, dim3(kThreads), 0, st, a);
     AW_LAUNCHED();
     return GSWA_OK;
 }
