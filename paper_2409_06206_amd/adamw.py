@@ -4,6 +4,7 @@ The functions carry the names of the C entry points.  Tensors are checked (type,
 is an error, there is no fallback path.
 """
 import ctypes
+import struct
 
 import torch
 
@@ -24,6 +25,10 @@ class adamw_desc(ctypes.Structure):
 class adamw_tensor(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("p_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("weight_decay", ctypes.c_float)]
     _fields_ += [(k, ctypes.c_void_p) for k in ("p", "master", "g", "m", "v", "m_exp", "v_exp")]
+
+
+_ROW = struct.Struct("@qiif4x7Q")   # an adamw_tensor: filled in one go, a list of some hundred tensors is as long as a step
+assert _ROW.size == ctypes.sizeof(adamw_tensor)
 
 
 class adamw_plan_t(ctypes.Structure):
@@ -60,30 +65,37 @@ _CODES = {torch.float32: GSWA_F32, torch.bfloat16: GSWA_BF16}
 
 def _list(desc, tensors):
     """The C list of tensors and the index of the device they lie on."""
-    c, eight = Call(), desc.state_bits == 8
-    state = torch.uint8 if eight else torch.float32
+    eight, f32, u8 = desc.state_bits == 8, torch.float32, torch.uint8
+    state, device = u8 if eight else f32, None
     out = (adamw_tensor * len(tensors))()
+
+    def place(name, t, dtype, n):
+        if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or t.numel() < n:
+            raise ValueError(f"tensor {i}: {name} must be a contiguous tensor of at least {n} elements of {dtype} on GPU {device}, not {t.numel()} "
+                             f"of {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+        return t.data_ptr()
+
     for i, part in enumerate(tensors):
         if not _FIELDS.issuperset(part):
             raise ValueError(f"tensor {i}: unknown fields {sorted(set(part) - _FIELDS)}")
         p, g, master = part["p"], part["g"], part.get("master")
-        n, row = p.numel(), out[i]
+        n, p_code, g_code = p.numel(), _CODES.get(p.dtype), _CODES.get(g.dtype)
         if g.numel() != n:
             raise ValueError(f"tensor {i}: {n} parameters, {g.numel()} gradients")
-        if p.dtype not in _CODES or g.dtype not in _CODES:
+        if p_code is None or g_code is None:
             raise ValueError(f"tensor {i}: parameters and gradients must be float32 or bfloat16, not {p.dtype} and {g.dtype}")
-        try:
-            row.n, row.p_dtype, row.g_dtype, row.weight_decay = n, _CODES[p.dtype], _CODES[g.dtype], part.get("weight_decay", 0.0)
-            row.p, row.g = c.flat("p", p, p.dtype, n), c.flat("g", g, g.dtype, n)
-            row.m, row.v = c.flat("m", part["m"], state, n), c.flat("v", part["v"], state, n)
-            if master is not None:
-                row.master = c.flat("master", master, torch.float32, n)
-            if eight:
-                blocks = -(-n // BLOCK)
-                row.m_exp, row.v_exp = c.flat("m_exp", part["m_exp"], torch.uint8, blocks), c.flat("v_exp", part["v_exp"], torch.uint8, blocks)
-        except ValueError as e:
-            raise ValueError(f"tensor {i}: {e}") from None
-    return out, c.device
+        if device is None:
+            device = p.get_device()
+            if device < 0:
+                raise ValueError(f"tensor {i}: p must lie on a GPU")
+        m_exp = v_exp = 0
+        if eight:
+            blocks = -(-n // BLOCK)
+            m_exp, v_exp = place("m_exp", part["m_exp"], u8, blocks), place("v_exp", part["v_exp"], u8, blocks)
+        _ROW.pack_into(out, i * _ROW.size, n, p_code, g_code, part.get("weight_decay", 0.0), place("p", p, p.dtype, n),
+                       0 if master is None else place("master", master, f32, n), place("g", g, g.dtype, n),
+                       place("m", part["m"], state, n), place("v", part["v"], state, n), m_exp, v_exp)
+    return out, device
 
 
 class Plan:

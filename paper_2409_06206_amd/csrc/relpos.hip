@@ -6,6 +6,7 @@
 #include "profile.h"
 
 #include <math.h>
+#include <type_traits>
 #include <vector>
 
 namespace gswa {
@@ -245,24 +246,31 @@ template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(TH
 // addition, in the same order every run, wherever its bucket's borders lie; only the sums of a tile's diagonals, some 64 V, are sorted into buckets, and most
 // tiles meet one bucket alone.
 
-// V columns of dout from column j on; zeros from column k on (k >= V: the vector that would reach over it is read V columns before it and moved)
+// V columns of dout from column j on.  The vector that reaches over a row's end is read with what stands behind it, in the last row of all, where there may
+// be nothing, V columns before the end; keep() takes away what is not the row's.  That is done when the values are used and not before: the loads stay in flight.
 template <typename T, int V> struct Columns {
     uint4 w;
-    __device__ __forceinline__ void load(const T *row, int j, int k, bool edge)
+    static __device__ __forceinline__ int place(int j, int k, bool last) { return last ? (j < k - V ? j : k - V) : j < k ? j : k - 1; }
+    __device__ __forceinline__ void load(const T *p)
     {
+        if constexpr (V == 1) w.x = sizeof(T) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t *>(p) : *reinterpret_cast<const uint32_t *>(p);
+        else __builtin_memcpy(&w, p, 16);
+    }
+    __device__ __forceinline__ void keep(int j, int k, bool last)
+    {
+        constexpr int kBits = 8 * sizeof(T);
         if constexpr (V == 1) {
-            w = make_uint4(0, 0, 0, 0);
-            if (j < k) w.x = sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t *>(row)[j] : reinterpret_cast<const uint32_t *>(row)[j];
+            w.x = j < k ? w.x : 0u;
+        } else if (last) { // the columns from j on to the front, zeros behind them
+            const int bits = (j - place(j, k, true)) * kBits < 128 ? (j - place(j, k, true)) * kBits : 128;
+            const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
+            const uint64_t l = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
+            const uint64_t u = bits < 64 ? hi >> bits : 0;
+            w = make_uint4((uint32_t)l, (uint32_t)(l >> 32), (uint32_t)u, (uint32_t)(u >> 32));
         } else {
-            __builtin_memcpy(&w, row + (j < k - V ? j : k - V), 16);
-            if (edge) {
-                const int cut = j + V - k; // columns too many
-                const int bits = cut > 0 ? (cut < V ? cut : V) * (int)(8 * sizeof(T)) : 0;
-                const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
-                const uint64_t l = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
-                const uint64_t u = bits < 64 ? hi >> bits : 0;
-                w = make_uint4((uint32_t)l, (uint32_t)(l >> 32), (uint32_t)u, (uint32_t)(u >> 32));
-            }
+            const int bits = (k - j) * kBits; // that are the row's
+            const auto part = [&](uint32_t v, int from) { return bits >= from + 32 ? v : bits > from ? v & 0xffffffffu >> (from + 32 - bits) : 0u; };
+            w = make_uint4(part(w.x, 0), part(w.y, 32), part(w.z, 64), part(w.w, 96));
         }
     }
     __device__ __forceinline__ float at(int i) const
@@ -306,6 +314,8 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
         const T *rows = static_cast<const T *>(a.dout) + (((long)b * a.heads + h) * a.q + i0) * a.ld;
         const int i1 = a.q - i0 < R ? a.q - i0 : R, j = j0 + lane * V;
         const bool edge = j0 + kColumns > a.k;
+        const int inside = Columns<T, V>::place(j, a.k, false), before = Columns<T, V>::place(j, a.k, true);
+        const int last = b == a.batch - 1 && h == a.heads - 1 ? a.q - 1 - i0 : -1; // the last row of all, among these
         float acc[V] = {}, gone = 0.f;
         Columns<T, V> now[kAtOnce], next[kAtOnce];
         const auto fetch = [&](int i, Columns<T, V> (&c)[kAtOnce]) {
@@ -313,7 +323,7 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
             for (int r = 0; r < kAtOnce; ++r) {
                 c[r].w = make_uint4(0, 0, 0, 0);
                 // (a lane all of whose columns are hidden from these rows does without them)
-                if (i + r < i1 && !(a.causal && j > i0 + i + kAtOnce - 1 + a.start)) c[r].load(rows + (long)(i + r) * a.ld, j, a.k, edge);
+                if (i + r < i1 && !(a.causal && j > i0 + i + kAtOnce - 1 + a.start)) c[r].load(rows + (long)(i + r) * a.ld + (i + r == last ? before : inside));
             }
         };
         fetch(0, now);
@@ -334,6 +344,7 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
                     for (int e = V - 1; e > 0; --e) acc[e] = acc[e - 1];
                     acc[0] = dpp_move<0x138>(out); // (wave_shr 1: from the lane before; 0 into the first)
                 }
+                if (edge) now[r].keep(j, a.k, i + r == last);
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += now[r].at(e);
             }
