@@ -1,10 +1,10 @@
-"""Device-side plumbing around the binding: uploads numpy inputs as torch tensors, owns the
-output/scratch buffers of one layer and hands raw results back.  No arithmetic of the layer
-happens here."""
+"""Device-side plumbing around the bindings: uploads numpy inputs as torch tensors, owns the
+output/scratch buffers of one layer, of a sequence of layers or of a training step and hands raw
+results back.  No arithmetic of the layers happens here."""
 import numpy as np
 import torch
 
-from . import astl, gswa, synth
+from . import adamw, astl, gswa, lnorm, relpos, synth
 
 _PARAMS = ("w_qkv", "b_qkv", "w_proj", "b_proj", "table")
 
@@ -174,3 +174,89 @@ class DeviceStack:
         for l, g in enumerate(self.grads):
             out.update({f"{l}.d{k}": to_host(v) for k, v in g.items()})
         return out
+
+
+class DeviceTrainer:
+    """One training step of a sequence of whole layers with a LayerNorm at its end: ``forward`` leaves z = LN(stack(x)), ``backward`` takes
+    the loss's gradient ``dz`` to every parameter's, ``update`` is one AdamW step, clipped by the norm of all gradients.  bf16 parameters
+    have an fp32 copy.
+
+    ``edges``: the bias tables of the layers come from learned tables of buckets of offsets (see include/relpos.h); None: every row of
+    a table is learned.  Nothing is allocated or read back after ``set_params``, so a step can be captured into a graph."""
+
+    DECAYED = ("w_qkv", "w_proj", "w_fc1", "w_fc2")
+
+    def __init__(self, B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every=0, eps=1e-5, flags=0,
+                 device="cuda:0", dqk=0, edges=None, lr=2e-4, betas=(0.9, 0.999), adam_eps=1e-8, weight_decay=0.01, max_norm=1.0,
+                 state_bits=32, seed=0):
+        self.stack = DeviceStack(B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every, eps, flags,
+                                 device, dqk)
+        self.lr, self.weight_decay, self.max_norm = lr, weight_decay, max_norm
+        self.norm_desc = lnorm.make_desc(B * H * W, C, dtype, eps)
+        self.bias_desc = None if edges is None else relpos.make_desc(heads, edges, dtype, relpos.RELPOS_BIDIRECTIONAL, window=window)
+        self.adam_desc = adamw.make_desc(*betas, adam_eps, state_bits, seed=seed)
+        new = lambda *shape, dtype=self.stack.y.dtype: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+        self.z, self.stack.dy = new(B, H, W, C), new(B, H, W, C)
+        self.dz = None
+        self.grads = {"norm_w": new(C, dtype=torch.float32), "norm_b": new(C, dtype=torch.float32)}
+        for l, g in enumerate(self.stack.grads):
+            self.grads.update({f"{l}.{k}": v for k, v in g.items() if edges is None or k != "table"})
+            if edges is not None:
+                self.grads[f"{l}.buckets"] = new(self.bias_desc.buckets, heads, dtype=torch.float32)
+        self.norm_ws = new(lnorm.lnorm_query_bytes(self.norm_desc), dtype=torch.uint8)
+        self.bias_ws = None if edges is None else new(relpos.relpos_query_bytes(self.bias_desc) + 256, dtype=torch.uint8)
+        self.step = torch.zeros(1, dtype=torch.int64, device=device)
+        self.grad_norm = torch.zeros((), device=device)
+        self.params = self.masters = self.states = self.plan = None
+
+    def set_params(self, per_layer, norm_w, norm_b):
+        """per_layer: numpy parameters of each layer as synth.astl_params names them, with ``buckets`` in the place of ``table`` where
+        the tables come from buckets.  States start at zero."""
+        s = self.stack
+        named = {"norm_w": norm_w, "norm_b": norm_b}
+        for l, p in enumerate(per_layer):
+            named.update({f"{l}.{k}": v for k, v in p.items()})
+        self.params = {k: to_device(v, s.dtype, s.device) for k, v in named.items()}
+        s.params = [{k: self.params[f"{l}.{k}"] for k in p if k != "buckets"} for l, p in enumerate(per_layer)]
+        if self.bias_desc is not None:
+            for p, g in zip(s.params, s.grads):
+                p["table"] = torch.empty(g["table"].shape, dtype=s.y.dtype, device=s.device)
+        self.masters = {k: torch.from_numpy(np.ascontiguousarray(v, dtype=np.float32)).to(s.device)
+                        for k, v in named.items()} if s.dtype == "bf16" else {}
+        eight = self.adam_desc.state_bits == 8
+        self.states, tensors = {}, []
+        for k, p in self.params.items():
+            zeros = lambda n, dt: torch.zeros(n, dtype=dt, device=s.device)  # noqa: E731
+            st = {n: zeros(p.numel(), torch.uint8 if eight else torch.float32) for n in ("m", "v")}
+            if eight:
+                st.update({n: zeros(-(-p.numel() // adamw.BLOCK), torch.uint8) for n in ("m_exp", "v_exp")})
+            self.states[k] = st
+            tensors.append(dict(st, p=p, g=self.grads[k], weight_decay=self.weight_decay if k.split(".")[-1] in self.DECAYED else 0.0))
+            if self.masters:
+                tensors[-1]["master"] = self.masters[k]
+        buffer = torch.empty(adamw.adamw_query_bytes(self.adam_desc, tensors), dtype=torch.uint8, device=s.device)
+        self.plan = adamw.adamw_plan(self.adam_desc, tensors, buffer)
+
+    def set_inputs(self, x, dz=None):
+        self.stack.x = to_device(x, self.stack.dtype, self.stack.device)
+        self.dz = None if dz is None else to_device(dz, self.stack.dtype, self.stack.device)
+
+    def forward(self, stream=None):
+        s = self.stack
+        if self.bias_desc is not None:
+            for l, p in enumerate(s.params):
+                relpos.relpos_forward(self.bias_desc, self.params[f"{l}.buckets"], p["table"], stream)
+        s.forward(True, stream)
+        lnorm.lnorm_forward(self.norm_desc, s.y, None, self.params["norm_w"], self.params["norm_b"], self.z, None, stream)
+
+    def backward(self, stream=None):
+        s, g = self.stack, self.grads
+        lnorm.lnorm_backward(self.norm_desc, s.y, self.dz, self.params["norm_w"], None, s.dy, g["norm_w"], g["norm_b"], self.norm_ws, stream)
+        s.backward(stream)
+        if self.bias_desc is not None:
+            for l, p in enumerate(s.grads):
+                relpos.relpos_backward(self.bias_desc, p["table"], g[f"{l}.buckets"], self.bias_ws, stream)
+
+    def update(self, stream=None):
+        adamw.adamw_norm(self.plan, self.grad_norm, stream)
+        adamw.adamw_step(self.plan, self.step, self.lr, norm=self.grad_norm, max_norm=self.max_norm, stream=stream)
