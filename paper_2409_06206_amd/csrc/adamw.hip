@@ -710,11 +710,14 @@ int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream)
     fill(plan, &a);
     a.norm_out = norm;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    KernelTimer t(K_ADAMW_NORM, st);
     const unsigned grid = grid_of(plan->chunks, kNormBlocks);
-    if (plan->each == 1) hipLaunchKernelGGL(norm_kernel<1>, dim3(grid), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(norm_kernel<kMany>, dim3(grid), dim3(kThreads), 0, st, a);
-    AW_LAUNCHED();
+    {
+        KernelTimer t(K_ADAMW_NORM, st);
+        if (plan->each == 1) hipLaunchKernelGGL(norm_kernel<1>, dim3(grid), dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL(norm_kernel<kMany>, dim3(grid), dim3(kThreads), 0, st, a);
+        AW_LAUNCHED();
+    }
+    KernelTimer t(K_ADAMW_NORM, st);
     hipLaunchKernelGGL(norm_sum_kernel, dim3(1), dim3(kThreads), 0, st, a, (int)grid);
     AW_LAUNCHED();
     return GSWA_OK;

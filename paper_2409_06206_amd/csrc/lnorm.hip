@@ -109,8 +109,9 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v)
 }
 
 // The L lanes of a row, and what each holds of it: vector p of a lane is columns [column(p), column(p) + V).  The row's last vector ends
-// at column C: where C is no multiple of V it begins inside the one before it, whose columns it reads as well but does not own.  (So no load or store
-// is ever narrower than a vector; both lanes store the same values.)
+// at column C: where C is no multiple of V it begins inside the one before it, whose columns it reads as well but does not own.  (So no load is ever
+// narrower than a vector.  Within a wavefront the stores are not either: both lanes store the same values.  Across wavefronts a lane stores what it owns: in a
+// call that works in place the other one may have read its vector again after this one stored.)
 template <int L, int P, int V, int THREADS> struct Place {
     static constexpr int kBlock = THREADS, kGroups = kBlock / L, kWaves = kBlock / 64;
     int C, lane;
@@ -134,11 +135,21 @@ template <int L, int P, int V, int THREADS> struct Place {
 #pragma unroll
         for (int p = 0; p < P; ++p) r[p] = row ? load<T, V>(static_cast<const T *>(row) + column(p)) : all<T, V>(without);
     }
+    template <typename T> __device__ __forceinline__ void put(T *row, int p, const float *f) const
+    {
+        if (!any(p)) return;
+        if (L <= 64 || own(p, 0)) {
+            store<T, V>(row + column(p), f);
+        } else {
+#pragma unroll
+            for (int i = 1; i < V; ++i)
+                if (own(p, i)) from_f32(row[column(p) + i], f[i]);
+        }
+    }
     template <typename T> __device__ __forceinline__ void put(T *row, const float (&f)[P * V]) const
     {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (any(p)) store<T, V>(row + column(p), f + p * V);
+        for (int p = 0; p < P; ++p) put(row, p, f + p * V);
     }
     // Sums over the lanes of a row, of N values at once.  Rows of more than a wavefront go through LDS; `half` alternates between
     // the two halves of it, so that one barrier a sum is enough.
@@ -203,7 +214,7 @@ __global__ __launch_bounds__((fwd_threads<L>())) void lnorm_fwd_kernel(Args a)
                 for (int i = 0; i < V; ++i) u[p * V + i] += r[i];
                 const Raw<T, V> held = pack(u + p * V, Raw<T, V>{}); // the norm is of what is stored
                 unpack(held, u + p * V);
-                if (live && pl.any(p)) __builtin_memcpy(static_cast<T *>(a.sum) + row * a.ldr + pl.column(p), &held.w, V * sizeof(T));
+                if (live) pl.put(static_cast<T *>(a.sum) + row * a.ldr, p, u + p * V); // (exact: the values are of the type)
             }
         }
         if (base + stride < a.rows) fetch(row + stride);
