@@ -171,24 +171,35 @@ template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(TH
     constexpr int V = Vec::V, kColumns = THREADS * V, kLine = 128 / sizeof(T), kBefore = ALIGNED ? 0 : kLine;
     __shared__ __align__(16) Bits values[kColumns + kBefore + kMostFwdRows + 4];
     __shared__ Bits learned[2 * (RELPOS_MAX_EDGES + 1)];
-    __shared__ int edges[RELPOS_MAX_EDGES];
+    __shared__ int edges[2 * (RELPOS_MAX_EDGES + 1)]; // (behind the last edge none is ever reached)
     const int h = blockIdx.y;
+    int top = 1; // the largest power of two up to n
+    while (2 * top <= a.n) top *= 2;
     for (int b = threadIdx.x; b < a.buckets; b += THREADS) learned[b] = static_cast<const Bits *>(a.table)[(long)b * a.heads + h];
-    for (int e = threadIdx.x; e < a.n; e += THREADS) edges[e] = a.edges[e];
+    for (int e = threadIdx.x; e < 2 * top; e += THREADS) edges[e] = e < a.n ? a.edges[e] : 0x7fffffff;
     const int tiles_k = (a.k + (ALIGNED ? 0 : kLine - 1) + kColumns - 1) / kColumns;
     const long tiles = (long)((a.q + a.rows - 1) / a.rows) * tiles_k;
     for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int i0 = (int)(tile / tiles_k) * a.rows, j0 = (int)(tile % tiles_k) * kColumns;
         const int i1 = i0 + a.rows < a.q ? i0 + a.rows : a.q, R = i1 - i0;
         __syncthreads();
-        const int count = kColumns + kBefore + R - 1, mine = (count + THREADS - 1) / THREADS, lowest = j0 - kBefore - (i1 - 1) - a.start;
-        int n = -1;
-        for (int x = threadIdx.x * mine; x < (int)(threadIdx.x + 1) * mine && x < count; ++x) {
-            const int r = lowest + x, d = r < 0 ? -r : a.bidirectional ? r : 0;
-            if (n < 0) n = edges_up_to(edges, a.n, d);
-            while (n > 0 && edges[n - 1] > d) --n;
-            while (n < a.n && edges[n] <= d) ++n;
-            values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n + a.n + 1 : n];
+        const int count = kColumns + kBefore + R - 1, lowest = j0 - kBefore - (i1 - 1) - a.start;
+        // all of a thread's offsets are searched for side by side: one chain of a few reads of LDS, not one for each
+        constexpr int kMine = (kColumns + kBefore + kMostFwdRows + THREADS - 1) / THREADS;
+        int n[kMine];
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) n[k] = 0;
+        for (int step = top; step; step >>= 1) {
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int r = lowest + (int)threadIdx.x + k * THREADS, d = r < 0 ? -r : a.bidirectional ? r : 0;
+                n[k] += edges[n[k] + step - 1] <= d ? step : 0;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int x = threadIdx.x + k * THREADS, r = lowest + x;
+            if (x < count) values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n[k] + a.n + 1 : n[k]];
         }
         __syncthreads();
         const int c = threadIdx.x * V;
