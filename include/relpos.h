@@ -13,7 +13,7 @@
  *   sequence (window == 0)   query i stands at position q_start + i, key j at j:
  *     out[h, i, j]  = table[bucket(j - i - q_start), h]           [heads, q_len, k_len], for all images of a batch
  *     dtable[b, h]  = sum over batch, i, j of that bucket of dout[batch, h, i, j]
- *     With RELPOS_CAUSAL keys behind the query get -infinity, and the gradients there are not read.
+ *     With RELPOS_CAUSAL keys behind the query get -infinity, and the gradients there take no part, whatever they hold.
  *     q_len = 1 is the step of a decoder: one query against k_len cached keys.
  *   window (window = M > 0)  the bias table of a GSWA layer with M x M windows from a table of buckets per axis,
  *     B = 2 (n_edges + 1) of them (RELPOS_BIDIRECTIONAL is required; the sequence fields are ignored):

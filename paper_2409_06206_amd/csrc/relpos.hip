@@ -27,18 +27,6 @@ struct Args {
     int edges[RELPOS_MAX_EDGES];
 };
 
-// edges <= d
-template <typename E> __device__ __forceinline__ int edges_up_to(const E *edges, int n, int d)
-{
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (edges[mid] <= d) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
 // ---- the table of a window --------------------------------------------------------------------------------------------------------
 // A few thousand values: what counts is the chain of dependent steps.  The buckets of the 2 M - 1 offsets of an axis are found side by side and kept
 // in LDS; a pair of buckets is a rectangle of offsets, which one workgroup sums.
@@ -88,6 +76,7 @@ __global__ __launch_bounds__(kThreads) void window_bwd_kernel(Args a)
         const int h = h0 + threadIdx.x % heads;
         float s = 0.f;
         if (slot < slots && h < a.heads)
+#pragma unroll 4
             for (int p = slot; p < places; p += slots) {
                 const int r = p / width;
                 s += dout[((long)(r0 + r) * side + c0 + (p - r * width)) * a.heads + h];
@@ -105,8 +94,8 @@ __global__ __launch_bounds__(kThreads) void window_bwd_kernel(Args a)
 }
 
 // ---- the bias of a sequence -------------------------------------------------------------------------------------------------------
-// Bound by the writes of the bias.  out[h, i, j] depends on j - i: a tile of R rows and C columns has R + C - 1 different values, which go to LDS once
-// (a thread finds the bucket of its first offset and walks on from there).  A lane writes the same V columns of every row; from one row to the next its
+// Bound by the writes of the bias.  out[h, i, j] depends on j - i: a tile of R rows and C columns has R + C - 1 different values, which go to LDS
+// once.  A lane writes the same V columns of every row; from one row to the next its
 // values move up by one place, so a row costs a lane one value out of LDS, a shift of its vector and one wide store.
 
 template <typename T> struct Vector;
