@@ -48,7 +48,7 @@ enum {
 
 typedef struct adamw_desc {
     double beta1, beta2; /* 0 <= beta < 1                                                                 */
-    float eps;          /* >= 0                                                                           */
+    float eps;          /* 0, or at least 2^-126                                                          */
     int32_t state_bits; /* 32 or 8                                                                        */
     uint32_t flags;
     uint64_t seed;      /* of the random roundings                                                        */
@@ -91,11 +91,13 @@ int adamw_query_bytes(const adamw_desc *desc, const adamw_tensor *tensors, int32
 int adamw_plan(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_tensors, void *buffer, adamw_plan_t *plan,
                void *hip_stream);
 
-/* *norm = sqrt(sum over all gradients of g^2), summed in fp64 and in a fixed order: the same bits every run. */
+/* *norm = sqrt(sum over all gradients of g^2), summed in fp64 and in a fixed order: the same bits every run.  A gradient that two tensors share
+ * counts twice. */
 int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream);
 
 /*
- * One step.  *step (device) is the number of steps taken so far and is raised by one, so that a captured step can be replayed.
+ * One step.  *step (device) is the number of steps taken so far, >= 0, and is raised by one, so that a captured step can be replayed: each plan
+ * has a counter of its own.  step, norm and lr_scale lie outside the tensors and the plan's buffer.
  *   lr        learning rate; with lr_scale (device, may be NULL) it is lr * *lr_scale
  *   norm      as adamw_norm leaves it (device), or NULL.  Where *norm > max_norm the gradients are taken times max_norm / *norm;
  *             max_norm = 0: no clipping, norm is then only looked at for ADAMW_SKIP_NONFINITE
@@ -106,7 +108,8 @@ int adamw_step(const adamw_plan_t *plan, int64_t *step, float lr, const float *l
 
 /*
  * What 8-bit states stand for, as bf16 (which holds them whole): m_out and v_out [elements] with every tensor starting at a
- * multiple of 256 and zeros from its end to the next start; plan->blocks * 256 elements each.  Either may be NULL.  GSWA_EINVAL for a plan of
+ * multiple of 256 and zeros from its end to the next start; plan->blocks * 256 elements each, disjoint
+ * from each other, from the tensors and from the plan's buffer.  Either may be NULL.  GSWA_EINVAL for a plan of
  * 32-bit states.
  */
 int adamw_unpack(const adamw_plan_t *plan, void *m_out, void *v_out, void *hip_stream);

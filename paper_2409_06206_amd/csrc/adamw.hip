@@ -22,10 +22,11 @@ constexpr int kStepBlocks = 65536;      // and of the others: a workgroup a piec
 constexpr int kGroups = 32;             // of the workgroups that are counted together (see last_of_all)
 constexpr int kCounterStep = 32;        // counters stand in lines of their own
 
-// Blocks of a piece of work that a wavefront takes at once: four for large lists, whose loads then keep the memory busy (read-back of 201 M elements: 234 us, with two
-// 308), one for small ones, where a wavefront's time counts (0.9 M elements in 468 tensors, 8-bit states: see kSmall).
+// Blocks of a piece of work that a wavefront takes at once.  Four for large lists, whose loads then keep the memory busy (201 M elements, 8-bit states: a step
+// 598 us and the read-back 218, with two blocks 672 and 308).  One for lists that do not fill the card, where the time of one wavefront counts (13 tensors
+// of a layer, 23 K elements: a step 5.6 us, with four 7.0; 0.9 M elements in 468 tensors: 9.9 us, with four 11).
 constexpr int kMany = 4;
-constexpr long kSmall = 8192;           // blocks of a list that is small: up to 2 M elements, 8 workgroups a compute unit
+constexpr long kSmall = 8192;           // blocks of a list that does not: up to 2 M elements, 8 workgroups a compute unit
 constexpr long chunk_of(int each) { return (long)kBlock * kWaves * each; }
 
 // A tensor as the kernels see it.
@@ -410,7 +411,7 @@ template <bool EIGHT, int N> __global__ __launch_bounds__(kThreads) void step_ke
         else if (T.master) by_gradient(std::integral_constant<int, kPBoth>{});
         else by_gradient(std::integral_constant<int, kP16>{});
     }
-    // (every workgroup has read the number of steps before)
+    __syncthreads(); // (all wavefronts of this workgroup have read the number of steps, with all others that have come here)
     if (threadIdx.x == 0 && last_of_all(a.counter)) *a.step += 1;
 }
 
@@ -542,7 +543,7 @@ template <int N> __global__ __launch_bounds__(kThreads) void unpack_kernel(Step 
 
 bool desc_ok(const adamw_desc *d)
 {
-    return d && d->beta1 >= 0. && d->beta1 < 1. && d->beta2 >= 0. && d->beta2 < 1. && d->eps >= 0.f && d->eps < INFINITY &&
+    return d && d->beta1 >= 0. && d->beta1 < 1. && d->beta2 >= 0. && d->beta2 < 1. && (d->eps == 0.f || d->eps >= 0x1p-126f) && d->eps < INFINITY &&
            (d->state_bits == 32 || d->state_bits == 8) && !(d->flags & ~(uint32_t)ADAMW_SKIP_NONFINITE);
 }
 
@@ -570,6 +571,9 @@ uint64_t checksum(const adamw_plan_t *p)
         h = (h ^ x) * 0x9E3779B97F4A7C15u, h ^= h >> 29;
     return h;
 }
+
+// the plan's own memory, which no other argument of a call may lie in
+Range buffer_of(const adamw_plan_t *p) { return Range(p->buffer, layout(p->n_tensors, p->chunks).bytes); }
 
 bool plan_ok(const adamw_plan_t *p) { return p && p->buffer && desc_ok(&p->desc) && p->check == checksum(p); }
 
@@ -705,7 +709,7 @@ int adamw_plan(const adamw_desc *desc, const adamw_tensor *tensors, int32_t n_te
 
 int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream)
 {
-    if (!plan_ok(plan) || !norm || !aligned_to(4, norm)) return GSWA_EINVAL;
+    if (!plan_ok(plan) || !norm || !aligned_to(4, norm) || overlaps_any(Range(norm, 4), buffer_of(plan))) return GSWA_EINVAL;
     Step a;
     fill(plan, &a);
     a.norm_out = norm;
@@ -727,6 +731,8 @@ int adamw_step(const adamw_plan_t *plan, int64_t *step, float lr, const float *l
                void *hip_stream)
 {
     if (!plan_ok(plan) || !step || !aligned_to(8, step) || !aligned_to(4, lr_scale, norm)) return GSWA_EINVAL;
+    if (overlaps_any(Range(step, 8), Range(norm, 4), Range(lr_scale, 4)) || overlaps_any(buffer_of(plan), Range(step, 8), Range(norm, 4), Range(lr_scale, 4)))
+        return GSWA_EINVAL;
     if (!(lr >= 0.f && lr < INFINITY) || !(max_norm >= 0.f && max_norm < INFINITY)) return GSWA_EINVAL;
     if ((max_norm > 0.f || (plan->desc.flags & ADAMW_SKIP_NONFINITE)) && !norm) return GSWA_EINVAL;
     Step a;
@@ -750,8 +756,8 @@ int adamw_unpack(const adamw_plan_t *plan, void *m_out, void *v_out, void *hip_s
 {
     if (!plan_ok(plan) || plan->desc.state_bits != 8 || (!m_out && !v_out) || !aligned_to(16, m_out, v_out)) return GSWA_EINVAL;
     const size_t bytes = (size_t)plan->blocks * kBlock * 2;
-    if (overlaps_any(Range(m_out, bytes), Range(v_out, bytes), Range(plan->buffer, layout(plan->n_tensors, plan->chunks).bytes)) ||
-        overlaps_any(Range(v_out, bytes), Range(plan->buffer, layout(plan->n_tensors, plan->chunks).bytes)))
+    if (overlaps_any(Range(m_out, bytes), Range(v_out, bytes), buffer_of(plan)) ||
+        overlaps_any(Range(v_out, bytes), buffer_of(plan)))
         return GSWA_EINVAL;
     if (!plan->chunks) return GSWA_OK;
     Step a;

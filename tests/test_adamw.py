@@ -51,7 +51,7 @@ def _plan(desc, parts, buffer=BASE - 256 * STEP):
     return adamw.lib().adamw_plan(ctypes.byref(desc), _c_tensors(*parts), len(parts), buffer, ctypes.byref(plan), None)
 
 
-@pytest.mark.parametrize("change", [dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(eps=float("inf")),
+@pytest.mark.parametrize("change", [dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(eps=float("inf")), dict(eps=2.0 ** -127),
                                     dict(state_bits=16), dict(flags=2)])
 def test_bad_descriptors(change):
     n = ctypes.c_size_t()
@@ -435,6 +435,43 @@ def test_a_plan_of_empty_tensors():
     adamw.adamw_norm(plan, norm)
     adamw.adamw_step(plan, step, 1e-3, norm=norm, max_norm=1.0)
     assert float(norm) == 0 and int(step) == 2
+
+
+@gpu
+def test_scalars_inside_the_plans_memory_are_refused():
+    parts = _device(_make([500], "f32", "f32", 32, 15))
+    plan, at = _planned(adamw.make_desc(), parts), None
+    step, norm = torch.tensor([4], device="cuda"), torch.ones(1, device="cuda")
+    at = plan.buffer.data_ptr()
+    before = plan.buffer.clone(), _cpu(parts)
+    for call in (lambda: adamw.adamw_norm(plan, at), lambda: adamw.adamw_step(plan, at + plan.buffer.numel() - 8, 1e-2),
+                 lambda: adamw.adamw_step(plan, step, 1e-2, norm=at, max_norm=1.0), lambda: adamw.adamw_step(plan, step, 1e-2, lr_scale=at),
+                 lambda: adamw.adamw_step(plan, step, 1e-2, norm=step.data_ptr() + 4, max_norm=1.0)):
+        with pytest.raises(gswa.GswaError):
+            call()
+    adamw.adamw_norm(plan, norm)
+    torch.cuda.synchronize()
+    assert int(step) == 4 and torch.equal(parts[0]["p"].cpu(), before[1][0]["p"])
+
+
+@gpu
+@pytest.mark.parametrize("sizes", [[1], [700], [4096], [1024] * 70], ids=str)
+def test_every_wavefront_of_a_step_sees_the_same_count(sizes):
+    """Steps right behind one another on tensors whose wavefronts end at different times: as with a wait after each of them."""
+    made = _make(sizes, "bf16", "f32", 8, 16, fresh=True)
+    desc, ends = adamw.make_desc(state_bits=8, seed=6), []
+    for wait in (False, True):
+        parts = _device(made)
+        plan, step = _planned(desc, parts), torch.tensor([0], device="cuda")
+        for _ in range(100):
+            adamw.adamw_step(plan, step, 1e-3)
+            if wait:
+                torch.cuda.synchronize()
+        assert int(step) == 100
+        ends.append(_cpu(parts))
+    for x, y in zip(*ends):
+        for name in ("p", "m", "v", "m_exp", "v_exp"):
+            assert torch.equal(x[name], y[name]), name
 
 
 @gpu
