@@ -41,8 +41,8 @@ typedef struct lnorm_desc {
     int64_t r_stride;  /* the same of residual, sum, dsum and dx                                         */
 } lnorm_desc;
 
-/* Scratch of lnorm_backward in bytes, a multiple of 256: a vector of 2 C partial sums for each of up to 1024
- * workgroups. lnorm_forward needs none. */
+/* Scratch of lnorm_backward in bytes, a multiple of 256: a vector of 2 C partial sums for each workgroup.
+ * lnorm_forward needs none. */
 int lnorm_query_bytes(const lnorm_desc *desc, size_t *bwd_ws_bytes);
 
 /*
