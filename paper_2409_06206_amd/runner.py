@@ -189,6 +189,8 @@ class DeviceTrainer:
     def __init__(self, B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every=0, eps=1e-5, flags=0,
                  device="cuda:0", dqk=0, edges=None, lr=2e-4, betas=(0.9, 0.999), adam_eps=1e-8, weight_decay=0.01, max_norm=1.0,
                  state_bits=32, seed=0):
+        if flags & gswa.GSWA_ACCUM_WGRAD:
+            raise ValueError("a step's gradients are its own: GSWA_ACCUM_WGRAD is not taken")
         self.stack = DeviceStack(B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every, eps, flags,
                                  device, dqk)
         self.lr, self.weight_decay, self.max_norm = lr, weight_decay, max_norm
@@ -211,7 +213,7 @@ class DeviceTrainer:
 
     def set_params(self, per_layer, norm_w, norm_b):
         """per_layer: numpy parameters of each layer as synth.astl_params names them, with ``buckets`` in the place of ``table`` where
-        the tables come from buckets.  States start at zero."""
+        the tables come from buckets.  States and the count of steps start at zero."""
         s = self.stack
         named = {"norm_w": norm_w, "norm_b": norm_b}
         for l, p in enumerate(per_layer):
@@ -223,6 +225,7 @@ class DeviceTrainer:
                 p["table"] = torch.empty(g["table"].shape, dtype=s.y.dtype, device=s.device)
         self.masters = {k: torch.from_numpy(np.ascontiguousarray(v, dtype=np.float32)).to(s.device)
                         for k, v in named.items()} if s.dtype == "bf16" else {}
+        self.step.zero_()
         eight = self.adam_desc.state_bits == 8
         self.states, tensors = {}, []
         for k, p in self.params.items():

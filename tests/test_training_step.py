@@ -159,3 +159,25 @@ def test_steps_on_two_streams():
     for a, b in zip(*sets):
         for k in a.params:
             assert torch.equal(a.params[k], b.params[k]), k
+
+
+def test_new_parameters_start_over():
+    t, layers, norm, _, _ = _trainer("bf16", 8)
+    t.forward()
+    t.backward()
+    ends = []
+    for _ in range(2):
+        for _ in range(3):
+            t.update()   # (on the same gradients: those of the layers are not the same bits every run)
+        assert int(t.step) == 3
+        ends.append({k: v.clone() for k, v in t.params.items()})
+        t.set_params(layers, *norm)
+        assert int(t.step) == 0
+    for k, v in ends[0].items():
+        assert torch.equal(v, ends[1][k]), k
+
+
+def test_gradients_added_up_over_steps_are_refused():
+    from paper_2409_06206_amd import gswa
+    with pytest.raises(ValueError, match="ACCUM"):
+        _trainer("f32", flags=gswa.GSWA_ACCUM_WGRAD)
