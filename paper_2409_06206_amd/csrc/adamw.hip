@@ -173,61 +173,110 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
     return r[0] > r[1] ? r[0] : r[1];
 }
 
-// Codes of a block.  Its exponent is the same for a wavefront, so what follows from it is kept in scalar registers: `base` is the pattern (upper 12 bits) of code 0.
-template <int TOP> __device__ __forceinline__ int base_of(int E) { return 8 * (E + 1) - TOP; }
-__device__ __forceinline__ uint32_t byte_of(uint32_t word, int j) { return word >> (8 * j) & 255u; }
+// Codes of a block.  Its exponent is the same for a wavefront (for half of one where it is read back), `base` the pattern (upper 12 bits) of code 0.  Codes
+// and patterns fit 16 bits, so two elements go through each operation: elements 0 and 2 of a lane in one register, 1 and 3 in another.  (A step with 8-bit
+// states and bf16 parameters without a copy is bound by its operations: 75 an element so, 94 with one element at a time.  201 M elements with bf16
+// gradients: 456 to 474 us, 514 to 519 before; 7.7 M: 26 us, 30.)
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 pair(uint32_t v) { return __builtin_bit_cast(u16x2, v); }
+__device__ __forceinline__ uint32_t word(u16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ u16x2 least(u16x2 a, uint16_t b) { return __builtin_elementwise_min(a, u16x2{b, b}); }
+__device__ __forceinline__ u16x2 most_signed(u16x2 a, int16_t b) // (patterns below 0 are met where a block holds next to nothing)
+{
+    return __builtin_bit_cast(u16x2, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a), i16x2{b, b}));
+}
+template <int TOP> __device__ __forceinline__ u16x2 base_of(int E)
+{
+    const uint16_t base = (uint16_t)(8 * (E + 1) - TOP);
+    return u16x2{base, base};
+}
+// 0 for 0, 1 for anything else (of the least with a plain 1 the compiler would make comparisons and choices, element by element)
+__device__ __forceinline__ u16x2 some(u16x2 a)
+{
+    uint32_t ones = 0x00010001u;
+    asm("" : "+s"(ones));
+    return __builtin_elementwise_min(a, pair(ones));
+}
+__device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// the magnitude's pattern that code c stands for (not of a block with E = 255)
-__device__ __forceinline__ uint32_t decode(uint32_t c, int base)
+// What four codes stand for, as bf16 patterns: elements 0 and 2, 1 and 3.
+__device__ __forceinline__ uint32_t decode(uint32_t codes, u16x2 base) // the magnitudes
 {
-    const int T = base + (int)c;
-    return c ? (uint32_t)(T > 1 ? T : 1) << 20 : 0u;
+    const u16x2 c = pair(codes);
+    return word(most_signed(c + base, 1) * some(c)) << 4;
 }
-__device__ __forceinline__ void decode_m(uint32_t word, int E, float (&m)[4])
+__device__ __forceinline__ u32x2 decode_m(uint32_t codes, int E)
 {
-    const int base = base_of<127>(E);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = __uint_as_float(decode(byte_of(word, j) & 127u, base) | (word << (24 - 8 * j) & 0x80000000u));
-    if (E == 255) m[0] = m[1] = m[2] = m[3] = __uint_as_float(0x7fc00000u);
+    const u16x2 base = base_of<127>(E);
+    const u32x2 q = {decode(codes & 0x007f007fu, base) | (codes << 8 & 0x80008000u), decode(codes >> 8 & 0x007f007fu, base) | (codes & 0x80008000u)};
+    return E == 255 ? u32x2{0x7fc07fc0u, 0x7fc07fc0u} : q;
 }
-__device__ __forceinline__ void decode_v(uint32_t word, int E, float (&v)[4])
+__device__ __forceinline__ u32x2 decode_v(uint32_t codes, int E)
 {
-    const int base = base_of<255>(E);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(decode(byte_of(word, j), base));
-    if (E == 255) v[0] = v[1] = v[2] = v[3] = __uint_as_float(0x7fc00000u);
+    const u16x2 base = base_of<255>(E);
+    const u32x2 q = {decode(codes & 0x00ff00ffu, base), decode(codes >> 8 & 0x00ff00ffu, base)};
+    return E == 255 ? u32x2{0x7fc07fc0u, 0x7fc07fc0u} : q;
+}
+__device__ __forceinline__ void as_floats(u32x2 q, float (&f)[4])
+{
+    f[0] = bf16_lo(q[0]); f[2] = bf16_hi(q[0]);
+    f[1] = bf16_lo(q[1]); f[3] = bf16_hi(q[1]);
+}
+__device__ __forceinline__ u32x2 in_order(u32x2 q) // four bf16 as they lie in memory
+{
+    return u32x2{__builtin_amdgcn_perm(q[1], q[0], 0x05040100u), upper_halves(q[0], q[1])};
 }
 
-// m's codes, the low 16 bits of h against what is cut off, and v's, the high ones (what is not 0 is not stored as 0)
+// bits + 16 times the lower or the upper half of h
+__device__ __forceinline__ uint32_t add_lower(uint32_t bits, uint32_t h)
+{
+    uint32_t r;
+    asm("v_mad_u32_u16 %0, %1, 16, %2" : "=v"(r) : "v"(h), "v"(bits));
+    return r;
+}
+__device__ __forceinline__ uint32_t add_upper(uint32_t bits, uint32_t h)
+{
+    uint32_t r;
+    asm("v_mad_u32_u16 %0, %1, 16, %2 op_sel:[1,0,0,0]" : "=v"(r) : "v"(h), "v"(bits));
+    return r;
+}
+
+// m's codes, the low 16 bits of h against what is cut off, and v's, the high ones (what is not 0 is not stored as 0).  Signs go along: nothing but a NaN
+// reaches them by the sum, and its block has E = 255.
 __device__ __forceinline__ uint32_t encode_m(const float (&m)[4], int E, const uint32_t (&h)[4])
 {
-    const int base = base_of<127>(E), most = E == 254 ? 126 : 127;
-    uint32_t word = 0;
+    const u16x2 base = base_of<127>(E);
+    const uint16_t most = E == 254 ? 126 : 127;
+    uint32_t t[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t bits = __float_as_uint(m[j]);
-        const int T = (int)(((bits & 0x7fffffffu) + ((h[j] & 0xffffu) << 4)) >> 20);
-        int c = T - base;
-        c = c < 0 ? 0 : c > most ? most : c;
-        if (T < 1) c = 0;
-        const uint32_t code = (uint32_t)c | (c ? bits >> 24 & 128u : 0u);
-        word |= code << (8 * j);
-    }
-    return E == 255 ? 0u : word;
+    for (int j = 0; j < 4; ++j) t[j] = add_lower(__float_as_uint(m[j]), h[j]);
+    const auto codes = [&](uint32_t x) {
+        const u16x2 T = pair(x >> 4 & 0x07ff07ffu), c = least(most_signed(T - base, 0), most) * some(T);
+        return word(pair(x >> 8 & 0x00800080u) * some(c) + c);
+    };
+    const uint32_t w = codes(upper_halves(t[0], t[2])) | codes(upper_halves(t[1], t[3])) << 8;
+    return E == 255 ? 0u : w;
 }
 __device__ __forceinline__ uint32_t encode_v(const float (&v)[4], int E, const uint32_t (&h)[4])
 {
-    const int base = base_of<255>(E), most = E == 254 ? 254 : 255;
-    uint32_t word = 0;
+    const u16x2 base = base_of<255>(E);
+    const uint16_t most = E == 254 ? 254 : 255;
+    uint32_t t[4], held[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t bits = __float_as_uint(v[j]) & 0x7fffffffu;
-        const int T = (int)((bits + ((h[j] >> 16) << 4)) >> 20);
-        int c = (T > 1 ? T : 1) - base;
-        c = c < 1 ? 1 : c > most ? most : c;
-        word |= (bits ? (uint32_t)c : 0u) << (8 * j);
+        const uint32_t bits = __float_as_uint(v[j]);
+        uint32_t one = 1u;
+        asm("" : "+s"(one));
+        t[j] = add_upper(bits, h[j]);
+        held[j] = bits < one ? bits : one;
     }
-    return E == 255 ? 0u : word;
+    const auto codes = [&](uint32_t x, uint32_t held) {
+        const u16x2 T = most_signed(pair(x >> 4 & 0x07ff07ffu), 1);
+        return word(least(most_signed(T - base, 1), most) * pair(held));
+    };
+    const uint32_t w = codes(upper_halves(t[0], t[2]), held[0] | held[2] << 16) | codes(upper_halves(t[1], t[3]), held[1] | held[3] << 16) << 8;
+    return E == 255 ? 0u : w;
 }
 
 // sqrt to a unit of its last place, of subnormal numbers too (the instruction takes those for 0)
@@ -324,8 +373,8 @@ __device__ __forceinline__ void step_blocks(const Step &a, const Rates &r, const
         floats(g4[k], g);
         floats(p4[k], p);
         if constexpr (EIGHT) {
-            decode_m(cm[k], __builtin_amdgcn_readfirstlane(em[k]), m);
-            decode_v(cv[k], __builtin_amdgcn_readfirstlane(ev[k]), v);
+            as_floats(decode_m(cm[k], __builtin_amdgcn_readfirstlane(em[k])), m);
+            as_floats(decode_v(cv[k], __builtin_amdgcn_readfirstlane(ev[k])), v);
         } else {
             floats(m4[k], m);
             floats(v4[k], v);
@@ -337,7 +386,7 @@ __device__ __forceinline__ void step_blocks(const Step &a, const Rates &r, const
             // (quotient and root to a unit of their last places: the update is some 1e-3 of the parameter)
             p[j] = p[j] * keep - r.rate * m[j] * __builtin_amdgcn_rcpf(root_of(v[j]) * r.root + a.eps);
             if constexpr (EIGHT) {
-                const uint32_t mb = __float_as_uint(m[j]) & 0x7fffffffu, vb = __float_as_uint(v[j]) & 0x7fffffffu;
+                const uint32_t mb = __float_as_uint(m[j]) & 0x7fffffffu, vb = __float_as_uint(v[j]); // (v is not negative, but for a NaN)
                 mmax = mb > mmax ? mb : mmax;
                 vmax = vb > vmax ? vb : vmax;
             }
@@ -364,7 +413,7 @@ __device__ __forceinline__ void step_blocks(const Step &a, const Rates &r, const
             store4<float, FULL>(at<float>(T.p, i), lane, left[k], patterns(p));
         }
         if constexpr (EIGHT) {
-            const int Em = __builtin_amdgcn_readfirstlane(wave_max(mmax) >> 23), Ev = __builtin_amdgcn_readfirstlane(wave_max(vmax) >> 23);
+            const int Em = __builtin_amdgcn_readfirstlane(wave_max(mmax) >> 23), Ev = __builtin_amdgcn_readfirstlane(wave_max(vmax) >> 23) & 255;
             if (lane == 0) {
                 ((Global<uint8_t> *)T.m_exp)[block] = (uint8_t)Em;
                 ((Global<uint8_t> *)T.v_exp)[block] = (uint8_t)Ev;
@@ -387,7 +436,7 @@ template <int N, typename F, typename H> __device__ __forceinline__ void each_bl
         if (b * kBlock < T.n) partly(b);
 }
 
-// Bound by memory: 16 to 30 bytes an element against about a hundred operations with 8-bit states, half of that with 32.  A wavefront has all loads of
+// Bound by memory, but with 8-bit states and no fp32 copy: 10 to 30 bytes an element against 70 operations with 8-bit states, half of that with 32.  A wavefront has all loads of
 // N blocks in flight together; a block's largest magnitude comes from exchanges between its lanes.
 template <bool EIGHT, int N> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
 {
@@ -484,10 +533,7 @@ template <int N, typename Decode>
 __device__ __forceinline__ void unpack_whole(const void *codes, const uint8_t *exp, uint16_t *out, long block, int lane, Decode decode)
 {
     if constexpr (N == 1) {
-        float f[4];
-        decode(((const Global<uint32_t> *)at<uint8_t>(codes, block * kBlock))[lane], ((const Global<uint8_t> *)exp)[block], f);
-        ((Global<u32x2> *)out)[lane] = u32x2{__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
-                                             __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xffff0000u)};
+        ((Global<u32x2> *)out)[lane] = in_order(decode(((const Global<uint32_t> *)at<uint8_t>(codes, block * kBlock))[lane], ((const Global<uint8_t> *)exp)[block]));
     } else {
         u32x2 c[N / 2];
         int E[N / 2];
@@ -498,12 +544,8 @@ __device__ __forceinline__ void unpack_whole(const void *codes, const uint8_t *e
         }
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) {
-            float lo[4], hi[4];
-            decode(c[k][0], E[k], lo);
-            decode(c[k][1], E[k], hi);
-            const u32x4 w = {__float_as_uint(lo[0]) >> 16 | (__float_as_uint(lo[1]) & 0xffff0000u), __float_as_uint(lo[2]) >> 16 | (__float_as_uint(lo[3]) & 0xffff0000u),
-                             __float_as_uint(hi[0]) >> 16 | (__float_as_uint(hi[1]) & 0xffff0000u), __float_as_uint(hi[2]) >> 16 | (__float_as_uint(hi[3]) & 0xffff0000u)};
-            ((Global<u32x4> *)at<uint16_t>((void *)out, 2 * k * kBlock))[lane] = w;
+            const u32x2 lo = in_order(decode(c[k][0], E[k])), hi = in_order(decode(c[k][1], E[k]));
+            ((Global<u32x4> *)at<uint16_t>((void *)out, 2 * k * kBlock))[lane] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
     }
 }
@@ -512,19 +554,17 @@ template <typename Decode> __device__ __forceinline__ void unpack_end(const void
 {
     const long over = n - block * kBlock - lane * 4;
     const int left = over < 0 ? 0 : over < 4 ? (int)over : 4;
-    float f[4];
-    decode(load4<uint8_t, false>(at<uint8_t>(codes, block * kBlock), lane, left), ((const Global<uint8_t> *)exp)[block], f);
-    uint32_t u[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) u[j] = j < left ? __float_as_uint(f[j]) : 0u;
-    ((Global<u32x2> *)out)[lane] = u32x2{u[0] >> 16 | (u[1] & 0xffff0000u), u[2] >> 16 | (u[3] & 0xffff0000u)};
+    u32x2 q = in_order(decode(load4<uint8_t, false>(at<uint8_t>(codes, block * kBlock), lane, left), ((const Global<uint8_t> *)exp)[block]));
+    q[0] &= left > 1 ? 0xffffffffu : left ? 0x0000ffffu : 0u; // (in a block of NaN they are not)
+    q[1] &= left > 3 ? 0xffffffffu : left > 2 ? 0x0000ffffu : 0u;
+    ((Global<u32x2> *)out)[lane] = q;
 }
 
 template <int N> __global__ __launch_bounds__(kThreads) void unpack_kernel(Step a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const auto of_m = [](uint32_t word, int E, float (&f)[4]) { decode_m(word, E, f); };
-    const auto of_v = [](uint32_t word, int E, float (&f)[4]) { decode_v(word, E, f); };
+    const auto of_m = [](uint32_t codes, int E) { return decode_m(codes, E); };
+    const auto of_v = [](uint32_t codes, int E) { return decode_v(codes, E); };
     for (long chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         const Tensor T = a.tensors[a.owner[chunk]];
         each_block<N>(T, chunk, wave,
