@@ -15,12 +15,15 @@ namespace gswa {
 namespace {
 
 constexpr int kSumThreads = 1024, kSumColumns = 32;
+// Rounds of rows that one workgroup takes where it then has them all, and no second launch adds partial sums (bf16 rows of 768: 16 of them, two rounds, 6.8 us, with the
+// second launch 8.3; 32, four rounds, 9.0, with it 8.6).
+constexpr int kAlone = 2;
 constexpr int N_MAX = 3; // sums of a row that are formed at once
 
 struct Args {
     const void *x, *residual, *gamma, *beta, *dy, *dsum;
     void *y, *sum, *dx;
-    float *part;    // backward: [workgroups][2 C], null where no parameter gradients are wanted
+    float *part;    // backward: [workgroups][2 C], null where no parameter gradients are wanted or one workgroup has all rows
     float *dgamma, *dbeta;
     long rows, ldx, ldy, ldr;
     int C, accumulate, parts;
@@ -253,7 +256,7 @@ __global__ __launch_bounds__((bwd_threads(L, P * V, V))) void lnorm_bwd_kernel(A
 {
     using Pl = Place<L, P, V, bwd_threads(L, P * V, V)>;
     __shared__ float lds[2][N_MAX][Pl::kWaves];
-    const Pl pl(a.C);
+    Pl pl(a.C);
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy), *ds = static_cast<const T *>(a.dsum);
     const long stride = (long)gridDim.x * Pl::kGroups;
     long row = (long)blockIdx.x * Pl::kGroups + (Pl::kGroups == 1 ? 0 : threadIdx.x / L);
@@ -327,50 +330,63 @@ __global__ __launch_bounds__((bwd_threads(L, P * V, V))) void lnorm_bwd_kernel(A
         }
         if (live) pl.put(static_cast<T *>(a.dx) + row * a.ldr, u);
     }
-    if (!a.part) return;
-    float *out = a.part + (size_t)blockIdx.x * 2 * a.C;
-    if constexpr (Pl::kGroups > 1) {
-        // groups of a wavefront by exchanges between its lanes, then the wavefronts that hold the same columns one after the other in LDS
-        constexpr int kTurns = L <= 64 ? Pl::kWaves : Pl::kGroups;
-        __shared__ float acc[2][L * P * V];
-        const int turn = L <= 64 ? threadIdx.x >> 6 : threadIdx.x / L;
+    if (!a.dgamma) return;
+    asm("" : "+v"(pl.lane)); // (or the places of what follows would be found before the loop and held through it)
+    float *const out_g = a.part ? a.part + (size_t)blockIdx.x * 2 * a.C : a.dgamma, *const out_b = a.part ? out_g + a.C : a.dbeta;
+    const bool add = !a.part && a.accumulate;
+    if constexpr (L > 64 && Pl::kGroups > 1) { // the other wavefronts' sums to those of the first row
+        static_assert(L <= 64 || Pl::kGroups <= 2, "two rows at once");
+        __shared__ float other[2][L * P * V];
+        if ((int)threadIdx.x >= L) {
 #pragma unroll
-        for (int k = 0; k < P * V; ++k) {
-            if constexpr (L == 8) dg[k] = dpp_add<0x128>(dg[k]), db[k] = dpp_add<0x128>(db[k]); // (row_ror 8)
-            if constexpr (L <= 16) dg[k] = rows_add(dg[k]), db[k] = rows_add(db[k]);
-            if constexpr (L <= 32) dg[k] = halves_add(dg[k]), db[k] = halves_add(db[k]);
+            for (int k = 0; k < P * V; ++k) other[0][k * L + pl.lane] = dg[k], other[1][k * L + pl.lane] = db[k];
         }
-        for (int w = 0; w < kTurns; ++w) {
-            if (turn == w && (L > 64 || (threadIdx.x & 63) < L)) {
+        __syncthreads();
+        if ((int)threadIdx.x >= L) return;
 #pragma unroll
-                for (int k = 0; k < P * V; ++k) {
-                    const int at = k * L + pl.lane;
-                    acc[0][at] = w ? acc[0][at] + dg[k] : dg[k];
-                    acc[1][at] = w ? acc[1][at] + db[k] : db[k];
-                }
+        for (int k = 0; k < P * V; ++k) dg[k] += other[0][k * L + pl.lane], db[k] += other[1][k * L + pl.lane];
+    }
+    const auto leave = [&](float *out, float (&f)[P * V]) {
+        if constexpr (L <= 64) {
+            // Groups of a wavefront by exchanges between its lanes; then each wavefront lays its sums into LDS, and a thread adds up a column in their
+            // order.  (Columns that a row's last vector reads again have the same sums in both lanes.)
+            __shared__ __align__(16) float sums[Pl::kWaves][L * P * V];
+#pragma unroll
+            for (int k = 0; k < P * V; ++k) {
+                if constexpr (L == 8) f[k] = dpp_add<0x128>(f[k]); // (row_ror 8)
+                if constexpr (L <= 16) f[k] = rows_add(f[k]);
+                if constexpr (L <= 32) f[k] = halves_add(f[k]);
+            }
+            __syncthreads(); // (the sums before these have been read)
+            float *mine = sums[threadIdx.x >> 6];
+            if ((threadIdx.x & 63) < L) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    if (pl.any(p)) __builtin_memcpy(mine + pl.column(p), f + p * V, V * sizeof(float));
             }
             __syncthreads();
-        }
-        if (threadIdx.x < L) {
+            for (int c = threadIdx.x; c < a.C; c += Pl::kBlock) {
+                float s = sums[0][c];
 #pragma unroll
-            for (int k = 0; k < P * V; ++k) dg[k] = acc[0][k * L + pl.lane], db[k] = acc[1][k * L + pl.lane];
-        }
-        if (threadIdx.x >= L) return;
-    }
+                for (int w = 1; w < Pl::kWaves; ++w) s += sums[w][c];
+                out[c] = add ? out[c] + s : s;
+            }
+        } else {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        if (pl.any(p) && pl.own(p, 0)) { // a whole vector of its own
-            __builtin_memcpy(out + pl.column(p), dg + p * V, V * sizeof(float));
-            __builtin_memcpy(out + a.C + pl.column(p), db + p * V, V * sizeof(float));
-        } else if (pl.any(p)) {
+            for (int p = 0; p < P; ++p) {
+                if (!pl.any(p)) continue;
+                if (pl.own(p, 0) && !add) { // a whole vector of its own
+                    __builtin_memcpy(out + pl.column(p), f + p * V, V * sizeof(float));
+                } else {
 #pragma unroll
-            for (int i = 1; i < V; ++i)
-                if (pl.own(p, i)) {
-                    out[pl.column(p) + i] = dg[p * V + i];
-                    out[a.C + pl.column(p) + i] = db[p * V + i];
+                    for (int i = 0; i < V; ++i)
+                        if (pl.own(p, i)) out[pl.column(p) + i] = add ? out[pl.column(p) + i] + f[p * V + i] : f[p * V + i];
                 }
+            }
         }
-    }
+    };
+    leave(out_g, dg);
+    leave(out_b, db);
 }
 
 // The partial sums of kSumColumns columns: a slice of the workgroups per 32 threads, then the slices in their order.
@@ -436,7 +452,9 @@ int make_plan(const lnorm_desc *d, Plan *p)
         return (unsigned)(rounds < most ? rounds : most);
     };
     p->fwd_blocks = blocks(L > 256 ? L : 256, (L > 256 ? 4 : 8) * kSizingCus);
+    const long together = bwd_threads(L, values, p->lanes ? V : 1) / L; // rows of a workgroup at once
     p->bwd_blocks = blocks(bwd_threads(L, values, p->lanes ? V : 1), (L > 256 && values > 16 ? 1 : L <= 64 && V == 4 && values > 8 ? 3 : 2) * kSizingCus);
+    if (d->rows <= kAlone * together) p->bwd_blocks = 1;
     p->ws = to_256((size_t)p->bwd_blocks * 2 * d->C * sizeof(float));
     return GSWA_OK;
 }
@@ -548,7 +566,7 @@ int lnorm_backward(const lnorm_desc *desc, const void *x, const void *dy, const 
     a.x = x; a.dy = dy; a.gamma = gamma; a.dsum = dsum; a.dx = dx; a.dgamma = dgamma; a.dbeta = dbeta;
     a.rows = desc->rows; a.ldx = p.ldx; a.ldy = p.ldy; a.ldr = p.ldr; a.C = desc->C; a.eps = desc->eps;
     a.accumulate = (desc->flags & LNORM_ACCUM_WGRAD) != 0;
-    a.part = dgamma ? static_cast<float *>(ws) : nullptr;
+    a.part = dgamma && p.bwd_blocks > 1 ? static_cast<float *>(ws) : nullptr;
     a.parts = (int)p.bwd_blocks;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     {
@@ -557,7 +575,7 @@ int lnorm_backward(const lnorm_desc *desc, const void *x, const void *dy, const 
         else launch_type<bf16_t>(a, p, false, st);
         LN_LAUNCHED();
     }
-    if (dgamma) {
+    if (a.part) {
         KernelTimer t(K_LNORM_SUM, st);
         hipLaunchKernelGGL(lnorm_sum_kernel, dim3((2 * desc->C + kSumColumns - 1) / kSumColumns), dim3(kSumThreads), 0, st, a);
         LN_LAUNCHED();

@@ -281,6 +281,22 @@ def test_gradients_by_differences():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [1, 7, 60, 131, 180, 391, 768, 1531, 2048, 2999, 4100, 8192])
+def test_gradients_of_one_workgroup_and_of_several_are_added_up(C, dtype):
+    """From one row, that one workgroup has, to enough for several: what is added is the plain call's, rounded once more."""
+    for rows in (1, 2, 5, 16, 70, 300):
+        i = {k: v.cuda() for k, v in _inputs(rows, C, dtype, 30).items()}
+        ws = torch.empty(lnorm.lnorm_query_bytes(lnorm.make_desc(rows, C, dtype)), dtype=torch.uint8, device="cuda")
+        first = [torch.randn(C, device="cuda") for _ in range(2)]
+        plain, added, dx = [torch.full((C,), float("nan"), device="cuda") for _ in range(2)], [t.clone() for t in first], torch.empty_like(i["x"])
+        lnorm.lnorm_backward(lnorm.make_desc(rows, C, dtype), i["x"], i["dy"], i["gamma"], None, dx, *plain, ws)
+        lnorm.lnorm_backward(lnorm.make_desc(rows, C, dtype, flags=lnorm.LNORM_ACCUM_WGRAD), i["x"], i["dy"], i["gamma"], None, dx, *added, ws)
+        for p, f, t in zip(plain, first, added):
+            assert torch.equal(t, f + p), (rows, C)
+
+
+@gpu
 def test_other_streams_and_a_replayed_graph():
     """Two streams at once with buffers of their own; a captured pass replayed on new values between eager calls."""
     cases = []
