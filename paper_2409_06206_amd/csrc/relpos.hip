@@ -19,7 +19,7 @@ constexpr int kMostFwdRows = 64;  // rows of a tile of the bias, at most
 struct Args {
     const void *table, *dout;
     void *out;
-    float *dtable, *part; // part: [heads][slices][buckets]
+    float *dtable, *part; // part: [heads][slices][buckets], null where one workgroup has all of a head
     long ld;
     int heads, batch, q, k, start, window, buckets, bidirectional, causal, accumulate, n;
     int rows, grad_rows;  // of a tile of the bias and of the gradient
@@ -392,8 +392,12 @@ template <typename T, int V> __global__ __launch_bounds__(kThreads) void sequenc
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < a.buckets; b += kThreads)
-        a.part[((long)h * a.slices + blockIdx.x) * a.buckets + b] = (sums[0][b] + sums[1][b]) + (sums[2][b] + sums[3][b]);
+    for (int b = threadIdx.x; b < a.buckets; b += kThreads) {
+        const float s = (sums[0][b] + sums[1][b]) + (sums[2][b] + sums[3][b]);
+        float *out = a.dtable + (long)b * a.heads + h;
+        if (a.part) a.part[((long)h * a.slices + blockIdx.x) * a.buckets + b] = s;
+        else *out = a.accumulate ? *out + s : s;
+    }
 }
 
 // The workgroups' sums of a head: a thread per bucket and group of them, the groups in their order.
@@ -615,7 +619,7 @@ int relpos_backward(const relpos_desc *desc, const void *dout, float *dtable, vo
     if (overlaps_any(rt, rd, rw) || overlaps_any(rw, rd)) return GSWA_EINVAL;
     Args a;
     fill(desc, p, &a);
-    a.dout = dout; a.dtable = dtable; a.part = static_cast<float *>(ws);
+    a.dout = dout; a.dtable = dtable; a.part = p.slices > 1 ? static_cast<float *>(ws) : nullptr;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (desc->window > 0) {
         KernelTimer t(K_RELPOS_BWD, st);
@@ -630,6 +634,7 @@ int relpos_backward(const relpos_desc *desc, const void *dout, float *dtable, vo
         else launch_backward<bf16_t>(a, p, grid, st);
         RP_LAUNCHED();
     }
+    if (!a.part) return GSWA_OK; // (16 x 16 positions: 4.8 us, 7.1 with a second launch)
     KernelTimer t(K_RELPOS_SUM, st);
     hipLaunchKernelGGL(sequence_sum_kernel, dim3(desc->heads), dim3(1024), 0, st, a);
     RP_LAUNCHED();
