@@ -151,7 +151,7 @@ template <> struct Vector<float> {
 };
 
 // Rows that do not start at multiples of a 128-byte line: a wavefront's stores would cover lines in part (16 x 4096 x 4104: 3.8 TB/s, where 4096 columns reach
-// 5.6), so a lane's columns move with the row, back to the last line's start (m of them, the tile's ends with them), and its vector is read out of LDS
+// 5.6; 4.2 now), so a lane's columns move with the row, back to the last line's start (m of them, the tile's ends with them), and its vector is read out of LDS
 // anew; elements before a row's first aligned vector and behind its last one are stored one by one.
 template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
 {
