@@ -23,6 +23,7 @@ struct Args {
     long ld;
     int heads, batch, q, k, start, window, buckets, bidirectional, causal, accumulate, n;
     int rows, grad_rows;  // of a tile of the bias and of the gradient
+    int spread;           // logarithm of the XCDs over which the bands of rows of the bias are spread
     int slices;           // workgroups of a head in the sums of the gradient
     int edges[RELPOS_MAX_EDGES];
 };
@@ -150,15 +151,30 @@ template <> struct Vector<float> {
     static constexpr uint32_t kMinusInf = 0xff800000u;
 };
 
-// Rows that do not start at multiples of a 128-byte line: a wavefront's stores would cover lines in part (16 x 4096 x 4104: 3.8 TB/s, where 4096 columns reach
-// 5.6; 4.2 now), so a lane's columns move with the row, back to the last line's start (m of them, the tile's ends with them), and its vector is read out of LDS
-// anew; elements before a row's first aligned vector and behind its last one are stored one by one.
-template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
+// Where a row starts.
+enum {
+    kAligned, // at a 128-byte line
+    kJoined,  // anywhere, one row right behind the other
+    kApart,   // anywhere, with something between them
+    kSingle   // anywhere, one a head
+};
+
+// A line that is written in part costs more than its bytes, also if another instruction writes the rest soon after.  So neighbouring rows are one XCD's, and
+// where rows do not start at lines, a lane's columns move with the row to where lines start and its vector is read out of LDS anew:
+//   joined  forward; a row has the lines that start in it, the last one with the next row's first columns, whose values wait in `starts`, and one
+//           instruction writes it (16 x 4096 rows of 4001 in bf16: 5.1 TB/s; with a row's own vectors and then what reaches over its end 4.4, with rows
+//           as apart 4.3; rows of 4032 5.4)
+//   apart   back to the line that the row starts in; elements before the first aligned vector and behind the last one are stored one by one, by a lane
+//           each, of all rows at once
+//   single  as apart, by the lanes that have them in a vector (one token against 8190 keys: 4.8 us, as apart 5.9)
+template <typename T, int THREADS, int ROWS> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
 {
     typedef Vector<T> Vec;
     typedef typename Vec::Bits Bits;
-    constexpr int V = Vec::V, kColumns = THREADS * V, kLine = 128 / sizeof(T), kBefore = ALIGNED ? 0 : kLine;
-    __shared__ __align__(16) Bits values[kColumns + kBefore + kMostFwdRows + 4];
+    constexpr int V = Vec::V, kColumns = THREADS * V, kLine = 128 / sizeof(T), kBefore = ROWS == kApart || ROWS == kSingle ? kLine : 0, kMore = ROWS == kAligned ? 0 : kLine;
+    constexpr int kValues = kColumns + kMore + kMostFwdRows, kStarts = ROWS == kJoined ? kLine + kMostFwdRows : 0;
+    __shared__ __align__(16) Bits values[kValues + kStarts + 4];
+    [[maybe_unused]] const Bits *const starts = values + kValues;
     __shared__ Bits learned[2 * (RELPOS_MAX_EDGES + 1)];
     __shared__ int edges[2 * (RELPOS_MAX_EDGES + 1)]; // (behind the last edge none is ever reached)
     const int h = blockIdx.y;
@@ -166,34 +182,42 @@ template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(TH
     while (2 * top <= a.n) top *= 2;
     for (int b = threadIdx.x; b < a.buckets; b += THREADS) learned[b] = static_cast<const Bits *>(a.table)[(long)b * a.heads + h];
     for (int e = threadIdx.x; e < 2 * top; e += THREADS) edges[e] = e < a.n ? a.edges[e] : 0x7fffffff;
-    const int tiles_k = (a.k + (ALIGNED ? 0 : kLine - 1) + kColumns - 1) / kColumns;
-    const long tiles = (long)((a.q + a.rows - 1) / a.rows) * tiles_k;
+    const int tiles_k = (a.k + (kBefore ? kLine - 1 : 0) + kColumns - 1) / kColumns;
+    const int bands = (a.q + a.rows - 1) / a.rows, per = (bands + (1 << a.spread) - 1) >> a.spread; // bands of rows, and those of an XCD (workgroups go to them in turn)
+    const long tiles = (long)per * tiles_k << a.spread;
     for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int i0 = (int)(tile / tiles_k) * a.rows, j0 = (int)(tile % tiles_k) * kColumns;
+        const long t = tile >> a.spread;
+        const int down = t >> 32 ? (int)(t / tiles_k) : (int)((uint32_t)t / (uint32_t)tiles_k), band = (int)(tile & ((1 << a.spread) - 1)) * per + down;
+        if (band >= bands) continue;
+        const int i0 = band * a.rows, j0 = (int)(t - (long)down * tiles_k) * kColumns;
         const int i1 = i0 + a.rows < a.q ? i0 + a.rows : a.q, R = i1 - i0;
         __syncthreads();
-        const int count = kColumns + kBefore + R - 1, lowest = j0 - kBefore - (i1 - 1) - a.start;
         // all of a thread's offsets are searched for side by side: one chain of a few reads of LDS, not one for each
-        constexpr int kMine = (kColumns + kBefore + kMostFwdRows + THREADS - 1) / THREADS;
+        constexpr int kMine = (kValues + kStarts + THREADS - 1) / THREADS;
+        const int lowest = j0 - kBefore - (i1 - 1) - a.start, count = kColumns + kMore + R - 1;
+        const auto offset = [&](int x) { return kStarts && x >= kValues ? x - kValues - i1 - a.start : x + lowest; };
         int n[kMine];
 #pragma unroll
         for (int k = 0; k < kMine; ++k) n[k] = 0;
         for (int step = top; step; step >>= 1) {
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                const int r = lowest + (int)threadIdx.x + k * THREADS, d = r < 0 ? -r : a.bidirectional ? r : 0;
+                const int r = offset(threadIdx.x + k * THREADS), d = r < 0 ? -r : a.bidirectional ? r : 0;
                 n[k] += edges[n[k] + step - 1] <= d ? step : 0;
             }
         }
 #pragma unroll
         for (int k = 0; k < kMine; ++k) {
-            const int x = threadIdx.x + k * THREADS, r = lowest + x;
-            if (x < count) values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n[k] + a.n + 1 : n[k]];
+            const int x = threadIdx.x + k * THREADS, r = offset(x);
+            if (x < count || (kStarts && x >= kValues && x < kValues + kStarts))
+                values[x] = a.causal && r > 0 ? (Bits)Vec::kMinusInf : learned[a.bidirectional && r > 0 ? n[k] + a.n + 1 : n[k]];
         }
         __syncthreads();
         const int c = threadIdx.x * V;
         Bits *const first = static_cast<Bits *>(a.out) + ((long)h * a.q + i0) * a.ld + j0; // the tile's corner
-        if constexpr (ALIGNED) {
+        // elements from the last line's start up to this row's column j0, which is a multiple of a line
+        const auto into_line = [&](const Bits *row) { return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(Bits)) & (kLine - 1); };
+        if constexpr (ROWS == kAligned) {
             const int j = j0 + c;
             if (j >= a.k) continue;
             Vec v;
@@ -218,21 +242,57 @@ template <typename T, int THREADS, bool ALIGNED> __global__ __launch_bounds__(TH
                     v.shift(values[c + i - 1]);
                 }
             }
+        } else if constexpr (ROWS == kJoined) {
+            if (i0 == 0 && j0 == 0) { // what lies before the head's first line
+                const int ahead = (kLine - into_line(first)) & (kLine - 1);
+                for (int e = threadIdx.x; e < ahead; e += THREADS) first[e] = values[e + R - 1];
+            }
+            // the rows' last lines, side by side
+            for (int t = threadIdx.x; t < R * (kLine / V); t += THREADS) {
+                const int i = t / (kLine / V);
+                Bits *row = first + (long)i * a.ld;
+                const int ahead = (kLine - into_line(row)) & (kLine - 1), line = (a.k - 1 - ahead) / kLine * kLine - j0; // from the tile's first one on
+                const int col = line + ahead + t % (kLine / V) * V, left = a.k - j0 - col;                               // columns of this row from there on
+                if (line < 0 || line >= kColumns) continue;
+                if (i0 + i + 1 < a.q) {
+                    Bits e[V];
+#pragma unroll
+                    for (int k = 0; k < V; ++k) e[k] = k < left ? values[col + k + R - 1 - i] : starts[k - left + R - 1 - i];
+                    __builtin_memcpy(__builtin_assume_aligned(row + col, 16), e, 16);
+                } else {
+                    for (int k = 0; k < left && k < V; ++k) row[col + k] = values[col + k + R - 1 - i];
+                }
+            }
+            if (j0 + (c & -64 * V) >= a.k) continue; // (nothing for this wavefront)
+#pragma unroll 2
+            for (int i = 0; i < R; ++i) {
+                Bits *row = first + (long)i * a.ld;
+                const int ahead = (kLine - into_line(row)) & (kLine - 1);
+                const Vec v = Vec::from(values, c, ahead + R - 1 - i);
+                if (j0 + (c & -kLine) + ahead + kLine < a.k) *reinterpret_cast<uint4 *>(row + c + ahead) = v.w;
+            }
         } else {
 #pragma unroll 2
             for (int i = 0; i < R; ++i) {
-                Bits *row = first + (long)i * a.ld; // (of column j0, which is a multiple of a line)
-                const int m = (int)(reinterpret_cast<uintptr_t>(row) / sizeof(Bits)) & (kLine - 1), above = kLine + R - 1 - i;
-                const Vec v = Vec::from(values, c, above - m);
-                const int col = c - m;
-                if (j0 + col >= 0 && j0 + col + V <= a.k) *reinterpret_cast<uint4 *>(row + col) = v.w;
-                if (threadIdx.x < 2 * V) { // a lane an element
-                    const int o = m & (V - 1), head = threadIdx.x, last = ((a.k + o) & ~(V - 1)) - o - j0, tail = last + head - V;
-                    if (head < V) {
-                        if (j0 == 0 && o > 0 && head < V - o && head < a.k) row[head] = values[head + above];
-                    } else if (j0 + last >= 0 && last + m >= 0 && last + m < kColumns && j0 + tail < a.k) {
-                        row[tail] = values[tail + above];
-                    }
+                Bits *row = first + (long)i * a.ld;
+                const int m = into_line(row), col = c - m;
+                const Vec v = Vec::from(values, c, kLine + R - 1 - i - m);
+                if (j0 + col >= 0 && j0 + col + V <= a.k) {
+                    *reinterpret_cast<uint4 *>(row + col) = v.w;
+                } else if (ROWS == kSingle) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (j0 + col + e >= 0 && j0 + col + e < a.k) row[col + e] = (Bits)v.at(e);
+                }
+            }
+            for (int t = threadIdx.x; ROWS == kApart && t < R * 2 * V; t += THREADS) {
+                const int i = t / (2 * V), head = t % (2 * V);
+                Bits *row = first + (long)i * a.ld;
+                const int m = into_line(row), above = kLine + R - 1 - i, o = m & (V - 1), last = ((a.k + o) & ~(V - 1)) - o - j0, tail = last + head - V;
+                if (head < V) {
+                    if (j0 == 0 && o > 0 && head < V - o && head < a.k) row[head] = values[head + above];
+                } else if (j0 + last >= 0 && last + m >= 0 && last + m < kColumns && j0 + tail < a.k) {
+                    row[tail] = values[tail + above];
                 }
             }
         }
@@ -422,6 +482,7 @@ struct Plan {
     int buckets, V;            // V: columns of a lane
     bool narrow;               // workgroups of one wavefront for the bias
     int rows, grad_rows;       // of a tile of the bias and of the gradient
+    int spread;                // logarithm of the XCDs over which the bands of rows of the bias are spread
     int slices;
 };
 
@@ -466,6 +527,7 @@ int make_plan(const relpos_desc *d, Plan *p)
         p->narrow = across * ceil_div(d->q_len, 8) < 2 * kSizingCus || d->k_len <= 64 * wide;
         p->rows = kMostFwdRows;
         while (p->rows > 8 && across * ceil_div(d->q_len, p->rows) < 8 * kSizingCus) p->rows /= 2;
+        p->spread = ceil_div(d->q_len, p->rows) < 16 ? 0 : 3; // 8 XCDs (few bands: workgroups of none would outweigh it)
         // Its gradient: tiles of 32 rows, fewer where that leaves less than four a compute unit; 16 workgroups a compute unit, over the
         // heads, more than run at once (tiles near the diagonal take longer, hidden ones no time).
         const long images = (long)d->batch * ceil_div(d->k_len, 64L * p->V);
@@ -486,6 +548,7 @@ void fill(const relpos_desc *d, const Plan &p, Args *a)
     *a = Args{};
     a->heads = d->heads; a->batch = d->batch; a->q = d->q_len; a->k = d->k_len; a->start = d->q_start;
     a->window = d->window; a->buckets = p.buckets; a->ld = p.ld; a->slices = p.slices; a->rows = p.rows; a->grad_rows = p.grad_rows;
+    a->spread = p.spread;
     a->bidirectional = (d->flags & RELPOS_BIDIRECTIONAL) != 0;
     a->causal = (d->flags & RELPOS_CAUSAL) != 0;
     a->accumulate = (d->flags & RELPOS_ACCUM_WGRAD) != 0;
@@ -493,19 +556,22 @@ void fill(const relpos_desc *d, const Plan &p, Args *a)
     for (int i = 0; i < d->n_edges; ++i) a->edges[i] = d->edges[i];
 }
 
-template <typename T> void launch_forward(const Args &a, const Plan &p, hipStream_t st)
+template <typename T, int ROWS> void launch_forward(const Args &a, const Plan &p, hipStream_t st)
 {
     const int threads = p.narrow ? 64 : kThreads, line = 128 / (int)sizeof(T);
-    const bool aligned = p.ld % line == 0 && reinterpret_cast<uintptr_t>(a.out) % 128 == 0;
-    const long tiles = ceil_div(a.q, a.rows) * ceil_div((long)a.k + (aligned ? 0 : line - 1), threads * (16L / sizeof(T)));
+    const long tiles = (ceil_div(ceil_div(a.q, a.rows), 1 << a.spread) << a.spread) * ceil_div((long)a.k + (ROWS == kApart || ROWS == kSingle ? line - 1 : 0), threads * (16L / sizeof(T)));
     const dim3 grid((unsigned)(tiles < (1L << 20) ? tiles : 1L << 20), a.heads);
-    if (aligned) {
-        if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64, true>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads, true>), grid, dim3(kThreads), 0, st, a);
-    } else {
-        if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64, false>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads, false>), grid, dim3(kThreads), 0, st, a);
-    }
+    if (p.narrow) hipLaunchKernelGGL((sequence_fwd_kernel<T, 64, ROWS>), grid, dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((sequence_fwd_kernel<T, kThreads, ROWS>), grid, dim3(kThreads), 0, st, a);
+}
+
+template <typename T> void launch_forward(const Args &a, const Plan &p, hipStream_t st)
+{
+    const int line = 128 / (int)sizeof(T);
+    if (p.ld % line == 0 && reinterpret_cast<uintptr_t>(a.out) % 128 == 0) launch_forward<T, kAligned>(a, p, st);
+    else if (p.ld == a.k && a.k >= line && a.q >= 8) launch_forward<T, kJoined>(a, p, st); // (a line that starts in a row ends in it or the next; a head's last row is not joined)
+    else if (a.q == 1) launch_forward<T, kSingle>(a, p, st);
+    else launch_forward<T, kApart>(a, p, st);
 }
 
 template <typename T> void launch_backward(const Args &a, const Plan &p, dim3 grid, hipStream_t st)

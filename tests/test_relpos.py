@@ -156,6 +156,36 @@ def test_rows_apart(pad, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [31, 32, 33, 63, 64, 65, 66, 95, 127, 129, 200, 255, 257, 480, 511, 512, 513, 575, 1000, 1023, 1025, 1055, 1087, 1531, 2039, 2047, 2049,
+                               2111, 4097])
+def test_rows_right_behind_one_another_from_any_place(k, dtype):
+    """Rows that start anywhere in a line and run into the next one: every element once, nothing before the first and behind the last."""
+    edges = list(range(1, 120))   # (a bucket for each offset near the diagonal, which passes through all row ends here)
+    size = torch.tensor([], dtype=TYPE[dtype]).element_size()
+    for n, (heads, q) in enumerate(((3, 1), (1, 2), (2, 9), (2, 65), (1, 200))):
+        for start in (0, k - 40 if k > 40 else 3):
+            for place in ((0, 16, 48, 112) if q == 9 else (16 * (n + 1),)):   # bytes behind a line's start
+                d = relpos.make_desc(heads, edges, dtype, BI, q, k, start)
+                table = torch.randn(d.buckets, heads, generator=torch.Generator().manual_seed(k)).to(TYPE[dtype])
+                room = torch.full((heads * q * k + 512,), 77.0, dtype=TYPE[dtype], device="cuda")
+                first = 128 // size + place // size
+                assert room.data_ptr() % 128 == 0
+                relpos.relpos_forward(d, table.cuda(), room[first: first + heads * q * k])
+                want = oracle.sequence_forward(table, q, k, start, edges, True, False)
+                assert torch.equal(room[first: first + heads * q * k].cpu().view(heads, q, k), want), (heads, q, start, place)
+                assert bool((room[:first] == 77).all()) and bool((room[first + heads * q * k:] == 77).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("q", [1, 2, 7, 8])
+def test_few_rows_apart(q, dtype):
+    for k, pad in ((5, 2), (515, 1), (515, 61), (1027, 5), (2100, 76)):
+        _check(3, q, k, k - q if k > q else 0, LOG[32, 128, False], dtype, CAUSAL, batch=2, pad=pad)
+
+
+@gpu
 def test_heads_and_images():
     for heads, batch in ((1, 5), (17, 1), (64, 3)):
         _check(heads, 40, 300, 260, LOG[32, 128, True], "bf16", BI, batch=batch)
