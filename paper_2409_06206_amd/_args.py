@@ -11,10 +11,34 @@ DTYPES = {"f32": GSWA_F32, "bf16": GSWA_BF16}
 TORCH_DTYPES = {GSWA_F32: torch.float32, GSWA_BF16: torch.bfloat16}
 # (the handle alone: torch.cuda.current_stream() builds a stream object around it, 1.8 us of a call of 5)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def torch_dtype(code):
     return TORCH_DTYPES.get(code, torch.bfloat16)   # (a code that is none is refused by the library)
+
+
+class Specs(dict):
+    """What the calls of a descriptor need of their tensors, by the descriptor's bytes: found once, since a small call takes no longer than finding it."""
+
+    MOST = 1024
+
+    def __init__(self, find):
+        super().__init__()
+        self.find = find
+
+    def of(self, desc):
+        key = bytes(desc)
+        spec = self.get(key)
+        if spec is None:
+            if len(self) >= self.MOST:
+                self.clear()
+            spec = self[key] = self.find(desc)
+        return spec
+
+
+def row_spec(rows, length, stride):
+    return (rows, length), (stride, 1)
 
 
 class Call:
@@ -48,21 +72,25 @@ class Call:
             raise ValueError(f"{name} has {t.numel()} elements, {numel} are needed")
         return t.data_ptr()
 
-    def rows(self, name, t, dtype, rows, length, stride):
-        """Address of `rows` rows of `length` elements, `stride` apart: contiguous in any shape, or 2-D."""
+    def rows(self, name, t, dtype, spec):
+        """Address of rows as row_spec names them: contiguous in any shape, or 2-D."""
         if t is None or t.__class__ is int:
             return t
         if t.get_device() != self.device or t.dtype is not dtype:
             self._place(name, t, dtype)
-        if t.shape == (rows, length) and t.stride() == (stride, 1):
-            return t.data_ptr()
+        if t.shape != spec[0] or t.stride() != spec[1]:
+            self._other_rows(name, t, spec)
+        return t.data_ptr()
+
+    @staticmethod
+    def _other_rows(name, t, spec):
+        (rows, length), (stride, _) = spec
         if t.is_contiguous() and (stride == length or rows == 1):
             if t.numel() != rows * length or t.shape[-1] != length:
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, {rows} rows of {length} are needed")
         elif t.dim() != 2 or t.shape != (rows, length) or (length > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != stride):
             raise ValueError(f"{name} must be {rows} rows of {length} elements, {stride} apart; it has shape {tuple(t.shape)} "
                              f"and strides {t.stride()}")
-        return t.data_ptr()
 
     def run(self, fn, stream, *args):
         """fn(*args, stream) on the tensors' device."""
@@ -77,7 +105,7 @@ class Call:
             if stream.device_index != self.device:
                 raise ValueError(f"the stream belongs to device {stream.device_index}, the tensors lie on device {self.device}")
             stream = stream.cuda_stream
-        if torch.cuda.current_device() == self.device:
+        if _current_device() == self.device:
             status = fn(*args, stream)
             if status != GSWA_OK:
                 _check(status)

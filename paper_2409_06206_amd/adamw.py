@@ -103,6 +103,7 @@ class Plan:
 
     def __init__(self, tensors, buffer):
         self.c_plan, self.tensors, self.buffer, self.device = adamw_plan_t(), tensors, buffer, buffer.get_device()
+        self.c_ref = ctypes.byref(self.c_plan)
 
     @property
     def elements(self):
@@ -133,16 +134,16 @@ def adamw_plan(desc, tensors, buffer, stream=None):
 
 def adamw_norm(plan, norm, stream=None):
     c = Call(plan.device)
-    c.run(lib().adamw_norm, stream, ctypes.byref(plan.c_plan), c.flat("norm", norm, torch.float32, 1))
+    c.run(gswa.lib().adamw_norm, stream, plan.c_ref, c.flat("norm", norm, torch.float32, 1))
 
 
 def adamw_step(plan, step, lr, lr_scale=None, norm=None, max_norm=0.0, stream=None):
     c = Call(plan.device)
-    c.run(lib().adamw_step, stream, ctypes.byref(plan.c_plan), c.flat("step", step, torch.int64, 1), lr,
+    c.run(gswa.lib().adamw_step, stream, plan.c_ref, c.flat("step", step, torch.int64, 1), lr,
           c.flat("lr_scale", lr_scale, torch.float32, 1), c.flat("norm", norm, torch.float32, 1), max_norm)
 
 
 def adamw_unpack(plan, m_out, v_out, stream=None):
     c = Call(plan.device)
-    c.run(lib().adamw_unpack, stream, ctypes.byref(plan.c_plan), c.flat("m_out", m_out, torch.bfloat16, plan.elements),
+    c.run(gswa.lib().adamw_unpack, stream, plan.c_ref, c.flat("m_out", m_out, torch.bfloat16, plan.elements),
           c.flat("v_out", v_out, torch.bfloat16, plan.elements))

@@ -8,8 +8,8 @@ import ctypes
 import torch
 
 from . import gswa
-from ._args import DTYPES, Call, torch_dtype
-from .gswa import _check
+from ._args import DTYPES, Call, Specs, row_spec, torch_dtype
+from .gswa import GSWA_OK, _check
 
 EXPORTS = ("lnorm_query_bytes", "lnorm_forward", "lnorm_backward")
 LNORM_ACCUM_WGRAD = 1
@@ -50,23 +50,28 @@ def lnorm_query_bytes(desc):
     return n.value
 
 
+def _spec(desc):
+    n, C = ctypes.c_size_t(), desc.C
+    known = lib().lnorm_query_bytes(ctypes.byref(desc), ctypes.byref(n)) == GSWA_OK   # (a descriptor that is none is refused by the call)
+    return (torch_dtype(desc.dtype), C, row_spec(desc.rows, C, desc.x_stride or C), row_spec(desc.rows, C, desc.y_stride or C),
+            row_spec(desc.rows, C, desc.r_stride or C), n.value if known else 0)
+
+
+_specs = Specs(_spec)
+
+
 def lnorm_forward(desc, x, residual, gamma, beta, y, sum, stream=None):
     """residual and sum, gamma, beta may be None (see the header)."""
-    L, c = lib(), Call()
-    t, rows, C = torch_dtype(desc.dtype), desc.rows, desc.C
-    r = desc.r_stride or C
-    c.run(L.lnorm_forward, stream, ctypes.byref(desc), c.rows("x", x, t, rows, C, desc.x_stride or C),
-          c.rows("residual", residual, t, rows, C, r), c.flat("gamma", gamma, t, C), c.flat("beta", beta, t, C),
-          c.rows("y", y, t, rows, C, desc.y_stride or C), c.rows("sum", sum, t, rows, C, r))
+    t, C, rx, ry, rr, _ = _specs.of(desc)
+    c = Call()
+    c.run(gswa.lib().lnorm_forward, stream, ctypes.byref(desc), c.rows("x", x, t, rx), c.rows("residual", residual, t, rr),
+          c.flat("gamma", gamma, t, C), c.flat("beta", beta, t, C), c.rows("y", y, t, ry), c.rows("sum", sum, t, rr))
 
 
 def lnorm_backward(desc, x, dy, gamma, dsum, dx, dgamma, dbeta, ws, stream=None):
     """gamma, dsum, and dgamma with dbeta (and then ws) may be None."""
-    L, c = lib(), Call()
-    t, rows, C = torch_dtype(desc.dtype), desc.rows, desc.C
-    r = desc.r_stride or C
-    need = lnorm_query_bytes(desc) if torch.is_tensor(ws) else 0
-    c.run(L.lnorm_backward, stream, ctypes.byref(desc), c.rows("x", x, t, rows, C, desc.x_stride or C),
-          c.rows("dy", dy, t, rows, C, desc.y_stride or C), c.flat("gamma", gamma, t, C), c.rows("dsum", dsum, t, rows, C, r),
-          c.rows("dx", dx, t, rows, C, r), c.flat("dgamma", dgamma, torch.float32, C), c.flat("dbeta", dbeta, torch.float32, C),
+    t, C, rx, ry, rr, need = _specs.of(desc)
+    c, f32 = Call(), torch.float32
+    c.run(gswa.lib().lnorm_backward, stream, ctypes.byref(desc), c.rows("x", x, t, rx), c.rows("dy", dy, t, ry), c.flat("gamma", gamma, t, C),
+          c.rows("dsum", dsum, t, rr), c.rows("dx", dx, t, rr), c.flat("dgamma", dgamma, f32, C), c.flat("dbeta", dbeta, f32, C),
           c.flat("ws", ws, torch.uint8, need))

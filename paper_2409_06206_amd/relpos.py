@@ -8,8 +8,8 @@ import ctypes
 import torch
 
 from . import gswa
-from ._args import DTYPES, Call, torch_dtype
-from .gswa import _check
+from ._args import DTYPES, Call, Specs, row_spec, torch_dtype
+from .gswa import GSWA_OK, _check
 
 EXPORTS = ("relpos_log_edges", "relpos_query_bytes", "relpos_forward", "relpos_backward")
 RELPOS_BIDIRECTIONAL, RELPOS_CAUSAL, RELPOS_ACCUM_WGRAD = 1, 2, 4
@@ -70,27 +70,34 @@ def relpos_query_bytes(desc):
     return n.value
 
 
-def _bias(c, name, t, dtype, desc, images):
-    """[images * heads, q_len] rows of k_len, or the table of a window."""
+def _spec(desc):
+    """Types, elements of the table, what the bias and its gradient have to be (a number of elements, or rows), scratch."""
+    n, t, ld = ctypes.c_size_t(), torch_dtype(desc.dtype), desc.row_stride or desc.k_len
+    known = lib().relpos_query_bytes(ctypes.byref(desc), ctypes.byref(n)) == GSWA_OK   # (a descriptor that is none is refused by the call)
     if desc.window:
-        return c.flat(name, t, dtype, (2 * desc.window - 1) ** 2 * desc.heads)
-    ld = desc.row_stride or desc.k_len
-    if ld == desc.k_len or t is None or isinstance(t, int):
-        return c.flat(name, t, dtype, images * desc.heads * desc.q_len * desc.k_len)
-    return c.rows(name, t, dtype, images * desc.heads * desc.q_len, desc.k_len, ld)
+        bias = grad = (2 * desc.window - 1) ** 2 * desc.heads
+    else:
+        rows = desc.heads * desc.q_len
+        bias, grad = (k * rows * desc.k_len if ld == desc.k_len else row_spec(k * rows, desc.k_len, ld) for k in (1, desc.batch))
+    return t, torch.float32 if desc.window else t, desc.buckets * desc.heads, bias, grad, n.value if known else 0
+
+
+_specs = Specs(_spec)
+
+
+def _bias(c, name, t, dtype, spec):
+    return c.flat(name, t, dtype, spec) if spec.__class__ is int else c.rows(name, t, dtype, spec)
 
 
 def relpos_forward(desc, table, out, stream=None):
-    L, c = lib(), Call()
-    t = torch_dtype(desc.dtype)
-    c.run(L.relpos_forward, stream, ctypes.byref(desc), c.flat("table", table, t, desc.buckets * desc.heads),
-          _bias(c, "out", out, t, desc, 1))
+    t, _, n, bias, _, _ = _specs.of(desc)
+    c = Call()
+    c.run(gswa.lib().relpos_forward, stream, ctypes.byref(desc), c.flat("table", table, t, n), _bias(c, "out", out, t, bias))
 
 
 def relpos_backward(desc, dout, dtable, ws, stream=None):
     """ws may be None where relpos_query_bytes is 0."""
-    L, c = lib(), Call()
-    need = relpos_query_bytes(desc) if torch.is_tensor(ws) else 0
-    c.run(L.relpos_backward, stream, ctypes.byref(desc),
-          _bias(c, "dout", dout, torch.float32 if desc.window else torch_dtype(desc.dtype), desc, desc.batch),
-          c.flat("dtable", dtable, torch.float32, desc.buckets * desc.heads), c.flat("ws", ws, torch.uint8, need))
+    _, t, n, _, grad, need = _specs.of(desc)
+    c = Call()
+    c.run(gswa.lib().relpos_backward, stream, ctypes.byref(desc), _bias(c, "dout", dout, t, grad), c.flat("dtable", dtable, torch.float32, n),
+          c.flat("ws", ws, torch.uint8, need))
