@@ -466,11 +466,14 @@ __global__ __launch_bounds__(1024) void sequence_sum_kernel(Args a)
     __shared__ double lds[1024];
     const int h = blockIdx.x, groups = 1024 / a.buckets, g = threadIdx.x / a.buckets, b = threadIdx.x - g * a.buckets;
     double s = 0.;
-    if (g < groups)
+    if (g < groups) {
+#pragma unroll 8
         for (int i = g; i < a.slices; i += groups) s += a.part[((long)h * a.slices + i) * a.buckets + b];
+    }
     lds[threadIdx.x] = s;
     __syncthreads();
     if (g) return;
+#pragma unroll 8
     for (int i = 1; i < groups; ++i) s += lds[i * a.buckets + b];
     float *out = a.dtable + (long)b * a.heads + h;
     *out = (float)(a.accumulate ? *out + s : s);
