@@ -18,6 +18,7 @@ constexpr int kSumThreads = 1024, kSumColumns = 32;
 // Rounds of rows that one workgroup takes where it then has them all, and no second launch adds partial sums (bf16 rows of 768: 16 of them, two rounds, 6.8 us, with the
 // second launch 8.3; 32, four rounds, 9.0, with it 8.6).
 constexpr int kAlone = 2;
+constexpr long kBalance = 500000; // see make_plan
 constexpr int N_MAX = 3; // sums of a row that are formed at once
 
 struct Args {
@@ -414,7 +415,7 @@ struct Plan {
     size_t elem, ws;
     long ldx, ldy, ldr;
     int lanes, vectors; // L and P; lanes = 0: rows shorter than a vector
-    unsigned fwd_blocks, bwd_blocks;
+    unsigned fwd_blocks, bwd_blocks, sum_blocks; // sum_blocks: of the backward pass where it leaves partial sums
 };
 
 // Lanes of a row: as few as hold it in 24 values of bf16 or 16 of fp32 each, at most 512, which hold the widest rows in 32.  (Fewer lanes with more
@@ -454,8 +455,13 @@ int make_plan(const lnorm_desc *d, Plan *p)
     p->fwd_blocks = blocks(L > 256 ? L : 256, (L > 256 ? 4 : 8) * kSizingCus);
     const long together = bwd_threads(L, values, p->lanes ? V : 1) / L; // rows of a workgroup at once
     p->bwd_blocks = blocks(bwd_threads(L, values, p->lanes ? V : 1), (L > 256 && values > 16 ? 1 : L <= 64 && V == 4 && values > 8 ? 3 : 2) * kSizingCus);
-    if (d->rows <= kAlone * together) p->bwd_blocks = 1;
-    p->ws = to_256((size_t)p->bwd_blocks * 2 * d->C * sizeof(float));
+    // With partial sums a workgroup takes at least r rounds of rows, such that r round times are what writing and reading the sums takes, 16 C bytes a workgroup: r^2 =
+    // rounds C / kBalance (8192 values in bf16: 512 rows in 512 workgroups 21.8 us, in 128 to 171 16.8 to 18.3, in 86 20.5; fp32, 1024 rows 36.1 and 27).
+    const long rounds = (d->rows + together - 1) / together;
+    long r = 1;
+    while (r * r * kBalance < rounds * d->C) ++r;
+    p->sum_blocks = rounds <= kAlone ? 1 : (unsigned)((rounds + r - 1) / r < p->bwd_blocks ? (rounds + r - 1) / r : p->bwd_blocks);
+    p->ws = to_256((size_t)p->sum_blocks * 2 * d->C * sizeof(float));
     return GSWA_OK;
 }
 
@@ -463,8 +469,8 @@ template <typename T, int L, int P, int V> void launch(const Args &a, const Plan
 {
     const dim3 fwd(fwd_threads<L>()), bwd(bwd_threads(L, P * V, V));
     if (forward) hipLaunchKernelGGL((lnorm_fwd_kernel<T, L, P, V>), dim3(p.fwd_blocks), fwd, 0, st, a);
-    else if (a.dsum) hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, true>), dim3(p.bwd_blocks), bwd, 0, st, a);
-    else hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, false>), dim3(p.bwd_blocks), bwd, 0, st, a);
+    else if (a.dsum) hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, true>), dim3(a.parts), bwd, 0, st, a);
+    else hipLaunchKernelGGL((lnorm_bwd_kernel<T, L, P, V, false>), dim3(a.parts), bwd, 0, st, a);
 }
 
 // The numbers of vectors that lanes_of leads to: more than half of the most, but on 8 lanes, and up to 32 values on 512.
@@ -566,8 +572,8 @@ int lnorm_backward(const lnorm_desc *desc, const void *x, const void *dy, const 
     a.x = x; a.dy = dy; a.gamma = gamma; a.dsum = dsum; a.dx = dx; a.dgamma = dgamma; a.dbeta = dbeta;
     a.rows = desc->rows; a.ldx = p.ldx; a.ldy = p.ldy; a.ldr = p.ldr; a.C = desc->C; a.eps = desc->eps;
     a.accumulate = (desc->flags & LNORM_ACCUM_WGRAD) != 0;
-    a.part = dgamma && p.bwd_blocks > 1 ? static_cast<float *>(ws) : nullptr;
-    a.parts = (int)p.bwd_blocks;
+    a.part = dgamma && p.sum_blocks > 1 ? static_cast<float *>(ws) : nullptr;
+    a.parts = (int)(dgamma ? p.sum_blocks : p.bwd_blocks);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     {
         KernelTimer t(K_LNORM_BWD, st);

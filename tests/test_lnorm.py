@@ -91,6 +91,22 @@ def test_tensors_are_checked_against_the_descriptor():
         lnorm.lnorm_forward(d, x, None, None, None, x.clone(), None, stream=0)
 
 
+def test_what_a_descriptor_needs_follows_its_fields():
+    """Found once for a descriptor's values, not for the object: a changed one is another."""
+    d, other = lnorm.make_desc(4, 8, "bf16"), lnorm.make_desc(4, 8, "bf16")
+    first = lnorm._specs.of(d)
+    assert lnorm._specs.of(other) == first
+    d.rows, d.y_stride = 5, 16
+    spec = lnorm._specs.of(d)
+    assert spec[2][0] == (5, 8) and spec[3] == ((5, 8), (16, 1)) and spec[5] == lnorm.lnorm_query_bytes(d)
+    d.rows = 4
+    d.y_stride = 0
+    assert lnorm._specs.of(d) == first
+    for rows in range(1, 1500):   # not more of them than a program has in use
+        lnorm._specs.of(lnorm.make_desc(rows, 8, "f32"))
+    assert len(lnorm._specs) <= lnorm._specs.MOST
+
+
 # ---- on the GPU --------------------------------------------------------------------------------------------------------------------
 
 def _strided(t, stride):
