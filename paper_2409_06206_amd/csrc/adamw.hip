@@ -69,7 +69,7 @@ struct Step {
     double beta1, beta2;
     float lr, max_norm, b1, b1c, b2, b2c, eps; // beta and 1 - beta, each rounded once
     int eight, skip;
-    uint32_t seed_lo, seed_hi;
+    uint32_t seed_key;
     uint16_t *m_out, *v_out;
 };
 
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a)
     for (int c = threadIdx.x; c < chunks; c += kThreads) a.owner[t.first_chunk + c] = index;
 }
 
-__device__ __forceinline__ uint32_t mix(uint32_t x)
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;
     x *= 0x9E3779B9u;
@@ -294,20 +294,21 @@ struct Rates {
 };
 __device__ __forceinline__ Rates rates_of(const Step &a, float norm)
 {
-    const uint64_t t = (uint64_t)*a.step + 1;
-    double b1 = 1., b2 = 1., f1 = a.beta1, f2 = a.beta2; // beta^t by squares
+    const uint64_t steps = (uint64_t)*a.step;
+    const uint32_t t_lo = __builtin_amdgcn_readfirstlane((uint32_t)steps), t_hi = __builtin_amdgcn_readfirstlane((uint32_t)(steps >> 32));
+    const uint64_t t = ((uint64_t)t_hi << 32 | t_lo) + 1;
+    double b = 1., f = threadIdx.x & 1 ? a.beta2 : a.beta1; // beta^t by squares: of beta1 in the even lanes, of beta2 in the odd ones
     for (uint64_t e = t; e; e >>= 1) {
-        if (e & 1) b1 *= f1, b2 *= f2;
-        f1 *= f1;
-        f2 *= f2;
+        if (e & 1) b *= f;
+        f *= f;
     }
+    const int rest = __float_as_int((float)(1. - b));
     Rates r;
     r.lr = a.lr_scale ? a.lr * *a.lr_scale : a.lr;
-    r.rate = r.lr / (float)(1. - b1);
-    r.root = (float)(1. / sqrt(1. - b2));
+    r.rate = r.lr / __int_as_float(__builtin_amdgcn_readlane(rest, 0));
+    r.root = 1.f / sqrtf(__int_as_float(__builtin_amdgcn_readlane(rest, 1)));
     r.clip = a.max_norm > 0.f && norm > a.max_norm ? a.max_norm / norm : 1.f;
-    r.key = mix(mix(a.seed_hi ^ 0x510E527Fu) ^ a.seed_lo);
-    r.key = mix(mix(r.key ^ (uint32_t)(t >> 32)) ^ (uint32_t)t);
+    r.key = mix(mix(a.seed_key ^ (uint32_t)(t >> 32)) ^ (uint32_t)t);
     return r;
 }
 
@@ -631,7 +632,7 @@ void fill(const adamw_plan_t *p, Step *a)
     a->b1 = (float)a->beta1; a->b1c = (float)(1. - a->beta1); a->b2 = (float)a->beta2; a->b2c = (float)(1. - a->beta2);
     a->eight = p->desc.state_bits == 8;
     a->skip = (p->desc.flags & ADAMW_SKIP_NONFINITE) != 0;
-    a->seed_lo = (uint32_t)p->desc.seed; a->seed_hi = (uint32_t)(p->desc.seed >> 32);
+    a->seed_key = mix(mix((uint32_t)(p->desc.seed >> 32) ^ 0x510E527Fu) ^ (uint32_t)p->desc.seed);
 }
 
 // No writable array may share a byte with another array of the list or with the buffer, but for a gradient shared by tensors.
