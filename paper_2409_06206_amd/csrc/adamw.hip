@@ -17,6 +17,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBlock = 256;             // elements that share an exponent: four for each lane of a wavefront
 constexpr int kNormBlocks = 1024;       // workgroups of the norm, at most
+constexpr unsigned kAlone = 64;         // workgroups of the norm whose last one adds up what they leave (see norm_kernel)
 constexpr int kStepBlocks = 65536;      // and of the others: a workgroup a piece of work up to 268 M elements (201 M, fp32: 1042 us; 4096 workgroups that
                                         // go on to further pieces 1127 us, 16384 1082 us)
 constexpr int kGroups = 32;             // of the workgroups that are counted together (see last_of_all)
@@ -68,7 +69,7 @@ struct Step {
     float *norm_out;
     double beta1, beta2;
     float lr, max_norm, b1, b1c, b2, b2c, eps; // beta and 1 - beta, each rounded once
-    int eight, skip;
+    int eight, skip, alone;
     uint32_t seed_key;
     uint16_t *m_out, *v_out;
 };
@@ -476,8 +477,9 @@ __device__ __forceinline__ double block_sum(double v)
 }
 
 // Four squares are added in fp32 and go on in fp64, so no sum over many elements loses digits; where a square could overflow or be lost (the sum of four
-// is out of bounds or hardly above 0) they are formed in fp64 too.  A launch of its own adds up what the workgroups leave, in their order: in one launch, with the
-// last workgroup adding, each of them has to write its caches back first, and 792 of them took 16 us where the two launches take 10.
+// is out of bounds or hardly above 0) they are formed in fp64 too.  What the workgroups leave is added in their order: by the last of a few of them, by a launch
+// of its own after many.  For the last one each has to write its caches back first, which many wait for: norm and step of 36 workgroups 8.8 us, with the second
+// launch 11.6; of 144 both 11.6; the norm of 792 alone 16 and 10.
 template <int N> __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -519,6 +521,17 @@ template <int N> __global__ __launch_bounds__(kThreads) void norm_kernel(Step a)
     }
     s = block_sum(s);
     if (threadIdx.x == 0) a.part[blockIdx.x] = s;
+    if (!a.alone) return;
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        last = arrived_last(a.counter, gridDim.x);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    }
+    __syncthreads();
+    if (!last) return;
+    s = block_sum(threadIdx.x < gridDim.x ? a.part[threadIdx.x] : 0.);
+    if (threadIdx.x == 0) *a.norm_out = (float)sqrt(s);
 }
 
 __global__ __launch_bounds__(kThreads) void norm_sum_kernel(Step a, int parts)
@@ -756,12 +769,14 @@ int adamw_norm(const adamw_plan_t *plan, float *norm, void *hip_stream)
     a.norm_out = norm;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const unsigned grid = grid_of(plan->chunks, kNormBlocks);
+    a.alone = grid <= kAlone;
     {
         KernelTimer t(K_ADAMW_NORM, st);
         if (plan->each == 1) hipLaunchKernelGGL(norm_kernel<1>, dim3(grid), dim3(kThreads), 0, st, a);
         else hipLaunchKernelGGL(norm_kernel<kMany>, dim3(grid), dim3(kThreads), 0, st, a);
         AW_LAUNCHED();
     }
+    if (a.alone) return GSWA_OK;
     KernelTimer t(K_ADAMW_NORM, st);
     hipLaunchKernelGGL(norm_sum_kernel, dim3(1), dim3(kThreads), 0, st, a, (int)grid);
     AW_LAUNCHED();

@@ -438,6 +438,29 @@ def test_a_plan_of_empty_tensors():
 
 
 @gpu
+@pytest.mark.parametrize("chunks", [1, 2, 63, 64, 65, 200, 1500])
+def test_norms_of_few_and_of_many_pieces(chunks):
+    """Added by the last workgroup or by a launch of its own: right, the same bits every run, replayed, and in turn with steps, which count on the same counters."""
+    made = _make([1024] * (chunks - 1) + [777], "f32", "f32", 32, chunks)
+    parts = _device(made)
+    plan, norm, step = _planned(adamw.make_desc(), parts), torch.zeros(1, device="cuda"), torch.tensor([0], device="cuda")
+    assert plan.c_plan.chunks == chunks
+    graph, replayed = torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        adamw.adamw_norm(plan, replayed)
+    for k in range(4):
+        for i, part in enumerate(parts):
+            part["g"].copy_(made[i]["g"] * (k + 1))
+        want = (k + 1) * math.sqrt(sum(float(b["g"].double().square().sum()) for b in made))
+        adamw.adamw_norm(plan, norm)
+        graph.replay()
+        adamw.adamw_step(plan, step, 0.0)
+        torch.cuda.synchronize()
+        assert abs(float(norm) - want) <= 4 * U * want and torch.equal(norm, replayed) and int(step) == k + 1   # (g (k + 1) is rounded: 2 U more)
+
+
+@gpu
 def test_scalars_inside_the_plans_memory_are_refused():
     parts = _device(_make([500], "f32", "f32", 32, 15))
     plan, at = _planned(adamw.make_desc(), parts), None
