@@ -534,3 +534,96 @@ def test_elements_beyond_2_to_32():
                                               ("v", v1, oracle.held_value(part["v"][cut].cpu(), part["v_exp"][lo // 256: -(-cut.stop // 256)].cpu(), True), 3, n_v)):
             x = x.expand(cut.stop - lo)
             _between(got, oracle.round_randomly(x * (1 - 32 * U), digits, noise16), oracle.round_randomly(x * (1 + 32 * U), digits, noise16), (name, lo))
+
+
+# ---- lists that fill the card: four blocks a wavefront -------------------------------------------------------------------------------
+
+# 8192 blocks are the most that a wavefront takes one at a time; the last ones end inside a wavefront's four blocks, inside a workgroup's sixteen and inside a block
+FULL = [2047 * 1024 + 1, 1, 256, 255, 1023, 1025, 0, 4096, 4097, 16 * 256 * 3 - 1, 70001]
+
+
+def test_lists_take_four_blocks_a_wavefront_from_8193_blocks_on():
+    """What the tests below rely on, in the plan's size: a number for each piece of work of 4 x 1 or 4 x 4 blocks."""
+    def size(blocks):
+        b = ctypes.c_size_t()
+        assert adamw.lib().adamw_query_bytes(ctypes.byref(adamw.make_desc()), _c_tensors(_part(n=256 * blocks)), 1, ctypes.byref(b)) == 0
+        return b.value
+
+    numbers = lambda pieces: -(-4 * pieces // 256) * 256  # noqa: E731
+    rest = size(4) - numbers(1)
+    assert size(8192) == rest + numbers(8192 // 4) and size(8193) == rest + numbers(-(-8193 // 16))
+    assert sum(-(-n // 256) for n in FULL) > 8192
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("p,g", KINDS)
+def test_steps_of_lists_that_fill_the_card(p, g, bits):
+    """As test_steps: a clipped step and one that is not, states of all kinds, nothing written behind a tensor's end."""
+    desc = adamw.make_desc(0.9, 0.999, 1e-8, bits, seed=0xFEDCBA987654321)
+    parts = _device(_make(FULL, p, g, bits, 21))
+    guard = []
+    for part in parts:
+        for k in ("p", "master", "m", "v", "m_exp", "v_exp"):
+            if k in part:
+                t = part[k]
+                wide = torch.empty(t.numel() + 64, dtype=t.dtype, device="cuda")
+                wide.view(torch.uint8).fill_(0xA5)
+                wide[: t.numel()] = t
+                part[k] = wide[: t.numel()]
+                guard.append((wide, t.numel()))
+    plan, step, norm = _planned(desc, parts), torch.tensor([40], device="cuda"), torch.zeros(1, device="cuda")
+    assert plan.c_plan.each == 4
+    for n in range(2):
+        before = _cpu(parts)
+        adamw.adamw_norm(plan, norm)
+        most = (float(norm) / 3, 0.0)[n]
+        adamw.adamw_step(plan, step, 1e-2, norm=norm, max_norm=most)
+        torch.cuda.synchronize()
+        want = math.sqrt(sum(float(b["g"].double().square().sum()) for b in before))
+        assert abs(float(norm) - want) <= 2 * U * want
+        _check_step(before, _cpu(parts), desc, 41 + n, 1e-2, most / want if n == 0 else 1.0)
+        assert int(step) == 41 + n
+    for wide, n in guard:
+        assert bool((wide[n:].view(torch.uint8) == 0xA5).all())
+
+
+@gpu
+def test_unpacked_states_of_a_list_that_fills_the_card():
+    """Two blocks a wavefront at once, each with an exponent of its own; blocks of NaN among them."""
+    made = _make(FULL, "bf16", "f32", 8, 22)
+    for i, at in ((0, 0), (0, 5), (0, 8187), (9, 2)):
+        made[i]["m_exp"][at] = 255
+        made[i]["v_exp"][at + 1] = 255
+    parts = _device(made)
+    plan = _planned(adamw.make_desc(state_bits=8), parts)
+    assert plan.c_plan.each == 4
+    m, v = (torch.full((plan.elements,), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    adamw.adamw_unpack(plan, m, v)
+    at = 0
+    for part in made:
+        n = part["p"].numel()
+        for out, k, second in ((m, "m", False), (v, "v", True)):
+            want = oracle.held_value(part[k], part[k + "_exp"], second)
+            assert torch.equal(out[at: at + n].double().cpu().nan_to_num(nan=123.0), want.nan_to_num(nan=123.0))
+            assert bool((out[at + n: at + -(-n // 256) * 256] == 0).all())
+        at += -(-n // 256) * 256
+    assert at == plan.elements
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_form_of_a_step_does_not_show_in_its_results(bits):
+    """A tensor's step is the same bits in a short list and in one that fills the card, its elements having the same numbers."""
+    made = _make([5000, 777, 2048, 1023], "bf16", "bf16", bits, 23)
+    rest = _make([8192 * 256], "bf16", "bf16", bits, 24)
+    desc, ends = adamw.make_desc(state_bits=bits, seed=31), []
+    for more in ([], rest):
+        parts = _device(made + more)
+        plan = _planned(desc, parts)
+        assert plan.c_plan.each == (4 if more else 1)
+        adamw.adamw_step(plan, torch.tensor([12], device="cuda"), 1e-2)
+        ends.append(_cpu(parts[: len(made)]))
+    for x, y in zip(*ends):
+        for k in set(x) - {"g", "weight_decay"}:
+            assert torch.equal(x[k], y[k]), k
