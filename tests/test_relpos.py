@@ -330,3 +330,79 @@ def test_other_streams_and_a_replayed_graph():
             run(d, table, dout, want)
             torch.cuda.synchronize()
             assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1]), k
+
+
+# ---- workgroups of 256 threads, tiles of many rows ---------------------------------------------------------------------------------
+
+def _check_forward(heads, q, k, start, edges, dtype, flags=0, pad=0, place=0, seed=0):
+    """All of the bias, held against the definition on the GPU (too much for the CPU); `place`: bytes behind a line's start."""
+    both, causal = bool(flags & BI), bool(flags & CAUSAL)
+    ld, size = k + pad, torch.tensor([], dtype=TYPE[dtype]).element_size()
+    d = relpos.make_desc(heads, edges, dtype, flags, q, k, start, row_stride=ld if pad else 0)
+    table = torch.randn(d.buckets, heads, generator=torch.Generator().manual_seed(seed)).to(TYPE[dtype]).cuda()
+    first, count = (128 + place) // size, heads * q * ld
+    room = torch.full((count + 512,), 77.0, dtype=TYPE[dtype], device="cuda")
+    assert room.data_ptr() % 128 == 0
+    rows = room[first: first + count].view(heads * q, ld)
+    relpos.relpos_forward(d, table, rows[:, :k] if pad else rows)
+    at = oracle.sequence_bucket(q, k, start, edges, both).cuda()
+    hidden = torch.arange(k, device="cuda")[None, :] > torch.arange(q, device="cuda")[:, None] + start
+    for h in range(heads):
+        want = table[:, h][at]
+        if causal:
+            want[hidden] = -math.inf
+        assert torch.equal(rows.view(heads, q, ld)[h, :, :k], want), h
+    assert bool((rows[:, k:] == 77).all())
+    assert bool((room[:first] == 77).all()) and bool((room[first + count:] == 77).all())
+
+
+# Workgroups have 256 threads where a row is longer than a wavefront's vectors (512 values in bf16, 256 in fp32) and 8 rows a tile make 512 of them or more.
+WIDE = {"bf16": (520, 1000, 1023, 1024, 1025, 2048, 2049, 2113, 4100), "f32": (260, 515, 1000, 1023, 1024, 1025, 1056, 2049, 2113)}
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", range(9))
+def test_workgroups_of_256_threads(n, dtype):
+    """Rows from a line's start, right behind one another from any place, and with something between them."""
+    k, near = WIDE[dtype][n], list(range(1, 120))
+    for heads, q, pad, place, flags in ((9, 512, 0, 0, BI), (9, 515, 0, 16, CAUSAL), (10, 483, 0, 112, BI), (9, 512, -k % 64, 0, BI), (9, 517, 1, 0, BI),
+                                        (9, 513, 3, 48, CAUSAL), (11, 480, 70, 16, 0)):
+        _check_forward(heads, q, k, k - 300 if n % 2 else 0, near, dtype, flags, pad, place, seed=n)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 5, None])   # None: rows that start at lines
+def test_tiles_of_64_rows(pad, dtype):
+    """Enough workgroups for the largest tiles, the last of which is short; bands of rows spread over the XCDs with some left over."""
+    k = 1025 if dtype == "f32" else 2049
+    _check_forward(33, 2027, k, 17, LOG[32, 128, True], dtype, BI, -k % 64 if pad is None else pad, seed=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,pad", [(600, 0), (640, 0), (601, 3), (2500, 0)])
+def test_one_token_of_many_heads(k, pad, dtype):
+    _check_forward(520, 1, k, k - 1, LOG[32, 128, False], dtype, CAUSAL, pad)
+    _check_forward(520, 3, k, k - 3, LOG[32, 128, False], dtype, CAUSAL, pad, 16)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,heads,q,k,start,pad", [
+    (2, 16, 512, 1531, 700, 0), (3, 16, 509, 1531, 0, 0), (2, 17, 515, 1536, 1021, 3), (2, 16, 1021, 640, 0, 0), (1, 40, 700, 2049, 1349, 0),   # tiles of 32 rows
+    (1, 16, 250, 1531, 700, 0), (1, 12, 333, 1400, 1, 1),                                                                                   # of 16 or 32
+    (1, 4, 333, 1100, 500, 0), (1, 1, 1000, 1000, 0, 0),                                                                                     # of 8 or 16
+])
+def test_gradients_of_a_causal_bias(batch, heads, q, k, start, pad, dtype):
+    """Hidden places hold NaN (see _check): none of it is seen, wherever the border passes through a tile."""
+    _check(heads, q, k, start, LOG[32, 128, False], dtype, CAUSAL, batch, pad, seed=heads)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("flags", [0, BI])
+def test_gradients_in_tiles_of_32_rows(flags, dtype):
+    _check(16, 517, 1531, 600, LOG[64, 800, True] if flags else LOG[128, 300, False], dtype, flags, batch=2, seed=5)
+    _check(12, 701, 2049, 0, list(range(1, 120)), dtype, flags, batch=2, pad=9, seed=6)
