@@ -369,3 +369,40 @@ def test_more_than_2_to_31_elements():
     assert torch.equal(db, torch.full((C,), float(rows), device="cuda"))   # whole numbers below 2^24: exact in any order
     # dy the same in all of a row: g - mean g = 0 and mean(g xh) = mean xh = 0 up to E
     assert float(y.abs().max()) < 64 * U * 16
+
+
+# ---- more rows than the workgroups take at once -----------------------------------------------------------------------------------
+
+# Workgroups of the forward pass: at most 1024 for rows on 512 lanes, 2048 for others, of 1 to 32 rows each; of the backward pass 256 to 768.
+ROUNDS = {"bf16": [(1100, 12289), (1031, 6150), (2100, 5001), (2053, 3080), (4200, 1539), (8300, 780), (17000, 333), (70001, 60)],
+          "f32": [(1100, 12289), (1031, 4100), (2100, 2501), (4200, 1531), (8300, 780), (17000, 333), (70001, 60)]}
+ROUNDS = [(dtype, rows, C) for dtype, shapes in ROUNDS.items() for rows, C in shapes]
+
+
+@gpu
+@pytest.mark.parametrize("dtype,rows,C", ROUNDS)
+@pytest.mark.parametrize("residual", [False, True])
+def test_workgroups_that_go_on_to_further_rows(dtype, rows, C, residual):
+    _check(rows, C, dtype, residual, seed=C)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,rows,C", ROUNDS)
+def test_in_place_over_further_rows(dtype, rows, C):
+    """The next row is read while this one's sum is stored: over x or the residual, and dx over dy or dsum, as into buffers of their own."""
+    i = {k: v.cuda() for k, v in _inputs(rows, C, dtype, 41).items()}
+    d = lnorm.make_desc(rows, C, dtype)
+    y, s, dx, y2 = (torch.empty_like(i["x"]) for _ in range(4))
+    lnorm.lnorm_forward(d, i["x"], i["residual"], i["gamma"], i["beta"], y, s)
+    assert torch.equal(s, (i["x"].float() + i["residual"].float()).to(TYPE[dtype]))
+    for over in ("x", "residual"):
+        j = {k: i[k].clone() for k in ("x", "residual")}
+        lnorm.lnorm_forward(d, j["x"], j["residual"], i["gamma"], i["beta"], y2, j[over])
+        assert torch.equal(y, y2) and torch.equal(s, j[over]), over
+    dg, db, dg2, db2 = (torch.empty(C, device="cuda") for _ in range(4))
+    ws = torch.empty(lnorm.lnorm_query_bytes(d), dtype=torch.uint8, device="cuda")
+    lnorm.lnorm_backward(d, s, i["dy"], i["gamma"], i["dsum"], dx, dg, db, ws)
+    for over in ("dy", "dsum"):
+        j = {k: i[k].clone() for k in ("dy", "dsum")}
+        lnorm.lnorm_backward(d, s, j["dy"], i["gamma"], j["dsum"], j[over], dg2, db2, ws)
+        assert torch.equal(dx, j[over]) and torch.equal(dg, dg2) and torch.equal(db, db2), over
