@@ -218,6 +218,11 @@ class DeviceTrainer:
         named = {"norm_w": norm_w, "norm_b": norm_b}
         for l, p in enumerate(per_layer):
             named.update({f"{l}.{k}": v for k, v in p.items()})
+        if set(named) != set(self.grads):
+            raise ValueError(f"parameters missing: {sorted(set(self.grads) - set(named))}, unknown: {sorted(set(named) - set(self.grads))}")
+        for k, v in named.items():
+            if np.size(v) != self.grads[k].numel():
+                raise ValueError(f"{k} has {np.size(v)} values, {self.grads[k].numel()} are needed")
         self.params = {k: to_device(v, s.dtype, s.device) for k, v in named.items()}
         s.params = [{k: self.params[f"{l}.{k}"] for k in p if k != "buckets"} for l, p in enumerate(per_layer)]
         if self.bias_desc is not None:
@@ -241,6 +246,9 @@ class DeviceTrainer:
         self.plan = adamw.adamw_plan(self.adam_desc, tensors, buffer)
 
     def set_inputs(self, x, dz=None):
+        for a in (x, dz):
+            if a is not None and np.size(a) != self.z.numel():
+                raise ValueError(f"{np.size(a)} values, {tuple(self.z.shape)} are needed")
         self.stack.x = to_device(x, self.stack.dtype, self.stack.device)
         self.dz = None if dz is None else to_device(dz, self.stack.dtype, self.stack.device)
 
