@@ -182,7 +182,8 @@ class DeviceTrainer:
     have an fp32 copy.
 
     ``edges``: the bias tables of the layers come from learned tables of buckets of offsets (see include/relpos.h); None: every row of
-    a table is learned.  Nothing is allocated or read back after ``set_params``, so a step can be captured into a graph."""
+    a table is learned.  A step allocates nothing and reads nothing back, so it can be captured into a graph; ``set_params`` and ``set_inputs``
+    wait for the steps under way and put new values where the old ones were, so a captured step goes on with them."""
 
     DECAYED = ("w_qkv", "w_proj", "w_fc1", "w_fc2")
 
@@ -199,7 +200,7 @@ class DeviceTrainer:
         self.adam_desc = adamw.make_desc(*betas, adam_eps, state_bits, seed=seed)
         new = lambda *shape, dtype=self.stack.y.dtype: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
         self.z, self.stack.dy = new(B, H, W, C), new(B, H, W, C)
-        self.dz = None
+        self._x, self._dz, self.dz = new(B, H, W, C), new(B, H, W, C), None
         self.grads = {"norm_w": new(C, dtype=torch.float32), "norm_b": new(C, dtype=torch.float32)}
         for l, g in enumerate(self.stack.grads):
             self.grads.update({f"{l}.{k}": v for k, v in g.items() if edges is None or k != "table"})
@@ -209,7 +210,7 @@ class DeviceTrainer:
         self.bias_ws = None if edges is None else new(relpos.relpos_query_bytes(self.bias_desc) + 256, dtype=torch.uint8)
         self.step = torch.zeros(1, dtype=torch.int64, device=device)
         self.grad_norm = torch.zeros((), device=device)
-        self.params = self.masters = self.states = self.plan = None
+        self.params = self.masters = self.states = self.plan = self.plan_buffer = None
 
     def set_params(self, per_layer, norm_w, norm_b):
         """per_layer: numpy parameters of each layer as synth.astl_params names them, with ``buckets`` in the place of ``table`` where
@@ -223,34 +224,60 @@ class DeviceTrainer:
         for k, v in named.items():
             if np.size(v) != self.grads[k].numel():
                 raise ValueError(f"{k} has {np.size(v)} values, {self.grads[k].numel()} are needed")
-        self.params = {k: to_device(v, s.dtype, s.device) for k, v in named.items()}
-        s.params = [{k: self.params[f"{l}.{k}"] for k in p if k != "buckets"} for l, p in enumerate(per_layer)]
-        if self.bias_desc is not None:
-            for p, g in zip(s.params, s.grads):
-                p["table"] = torch.empty(g["table"].shape, dtype=s.y.dtype, device=s.device)
-        self.masters = {k: torch.from_numpy(np.ascontiguousarray(v, dtype=np.float32)).to(s.device)
-                        for k, v in named.items()} if s.dtype == "bf16" else {}
-        self.step.zero_()
-        eight = self.adam_desc.state_bits == 8
-        self.states, tensors = {}, []
-        for k, p in self.params.items():
-            zeros = lambda n, dt: torch.zeros(n, dtype=dt, device=s.device)  # noqa: E731
-            st = {n: zeros(p.numel(), torch.uint8 if eight else torch.float32) for n in ("m", "v")}
-            if eight:
-                st.update({n: zeros(-(-p.numel() // adamw.BLOCK), torch.uint8) for n in ("m_exp", "v_exp")})
-            self.states[k] = st
-            tensors.append(dict(st, p=p, g=self.grads[k], weight_decay=self.weight_decay if k.split(".")[-1] in self.DECAYED else 0.0))
+        if self.params is None:
+            self._allocate(named, len(per_layer))
+        self._settle()
+        tensors = []
+        for k, v in named.items():
+            p, states = self.params[k], self.states[k]
+            p.copy_(to_device(v, s.dtype, "cpu").reshape(p.shape))
+            tensors.append(dict(states, p=p, g=self.grads[k], weight_decay=self.weight_decay if k.split(".")[-1] in self.DECAYED else 0.0))
             if self.masters:
                 tensors[-1]["master"] = self.masters[k]
-        buffer = torch.empty(adamw.adamw_query_bytes(self.adam_desc, tensors), dtype=torch.uint8, device=s.device)
-        self.plan = adamw.adamw_plan(self.adam_desc, tensors, buffer)
+                self.masters[k].copy_(to_device(v, "f32", "cpu").reshape(p.shape))
+            for state in states.values():
+                state.zero_()
+        self.step.zero_()
+        if self.plan_buffer is None:
+            self.plan_buffer = torch.empty(adamw.adamw_query_bytes(self.adam_desc, tensors), dtype=torch.uint8, device=s.device)
+        self.plan = adamw.adamw_plan(self.adam_desc, tensors, self.plan_buffer)
+        self._settle()
+
+    def _allocate(self, named, layers):
+        """What a step reads and writes of parameters and states."""
+        s, eight = self.stack, self.adam_desc.state_bits == 8
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=s.device)  # noqa: E731
+        self.params = {k: new(np.shape(v), s.y.dtype) for k, v in named.items()}
+        self.masters = {k: new(np.shape(v), torch.float32) for k, v in named.items()} if s.dtype == "bf16" else {}
+        s.params = [{k.split(".")[-1]: v for k, v in self.params.items() if k.startswith(f"{l}.") and not k.endswith(".buckets")}
+                    for l in range(layers)]
+        if self.bias_desc is not None:
+            for p, g in zip(s.params, s.grads):
+                p["table"] = new(g["table"].shape, s.y.dtype)
+        self.states = {}
+        for k, p in self.params.items():
+            n = p.numel()
+            self.states[k] = {m: new(n, torch.uint8 if eight else torch.float32) for m in ("m", "v")}
+            if eight:
+                self.states[k].update({m: new(-(-n // adamw.BLOCK), torch.uint8) for m in ("m_exp", "v_exp")})
+
+    def _settle(self):
+        """Values change when no step is under way, on whatever stream, and are there for the next one."""
+        if self.step.is_cuda:
+            torch.cuda.synchronize(self.step.device)
 
     def set_inputs(self, x, dz=None):
+        """Without dz there is nothing for ``backward`` to start from."""
+        s, shape = self.stack, self.z.shape
         for a in (x, dz):
             if a is not None and np.size(a) != self.z.numel():
-                raise ValueError(f"{np.size(a)} values, {tuple(self.z.shape)} are needed")
-        self.stack.x = to_device(x, self.stack.dtype, self.stack.device)
-        self.dz = None if dz is None else to_device(dz, self.stack.dtype, self.stack.device)
+                raise ValueError(f"{np.size(a)} values, {tuple(shape)} are needed")
+        self._settle()
+        s.x, self.dz = self._x, None if dz is None else self._dz
+        for t, a in ((s.x, x), (self.dz, dz)):
+            if a is not None:
+                t.copy_(to_device(a, s.dtype, "cpu").reshape(shape))
+        self._settle()
 
     def forward(self, stream=None):
         s = self.stack

@@ -2,8 +2,11 @@
 """
 import numpy as np
 import pytest
+import torch
 
 from paper_2409_06206_amd import synth
+
+gpu = pytest.mark.gpu
 
 B, H, W, C, HEADS, GROUPS, WINDOW, SHIFT, HIDDEN, LAYERS = 2, 16, 24, 60, 6, 2, 8, 4, 120, 2
 EDGES = [1, 2, 4]
@@ -28,6 +31,16 @@ def _new(dtype, device="cuda:0", edges=EDGES, **kw):
     return runner.DeviceTrainer(B, H, W, C, HEADS, GROUPS, WINDOW, SHIFT, dtype, HIDDEN, LAYERS, device=device, **kw)
 
 
+def _places(t):
+    """Address of every buffer that a step reads or writes."""
+    out = {"x": t.stack.x, "dz": t.dz, "z": t.z, "dy": t.stack.dy, "step": t.step, "grad_norm": t.grad_norm, "plan": t.plan.buffer}
+    out.update({f"params.{k}": v for k, v in t.params.items()})
+    out.update({f"masters.{k}": v for k, v in t.masters.items()})
+    out.update({f"states.{k}.{n}": v for k, st in t.states.items() for n, v in st.items()})
+    out.update({f"layers.{l}.{k}": v for l, p in enumerate(t.stack.params) for k, v in p.items()})
+    return {k: v.data_ptr() for k, v in out.items()}
+
+
 # ---- without a GPU ---------------------------------------------------------------------------------------------------------------
 
 @pytest.fixture
@@ -40,6 +53,45 @@ def on_cpu(monkeypatch):
             self.tensors, self.buffer = tensors, buffer
 
     monkeypatch.setattr(adamw, "adamw_plan", lambda desc, tensors, buffer, stream=None: Plan(tensors, buffer))
+
+
+@pytest.mark.parametrize("dtype,bits", [("f32", 32), ("bf16", 8)])
+def test_new_values_go_where_the_old_ones_were(on_cpu, dtype, bits):
+    """A captured step reads and writes the buffers it was captured with."""
+    t = _new(dtype, "cpu", state_bits=bits)
+    layers, norm, inputs = _values(dtype, 0)
+    t.set_params(layers, *norm)
+    t.set_inputs(*inputs)
+    first, grads = _places(t), {k: v.data_ptr() for k, v in t.grads.items()}
+    for st in t.states.values():
+        for v in st.values():
+            v.fill_(3)
+    t.step.fill_(9)
+    layers, norm, inputs = _values(dtype, 1)
+    t.set_params(layers, *norm)
+    t.set_inputs(*inputs)
+    assert _places(t) == first and {k: v.data_ptr() for k, v in t.grads.items()} == grads
+    assert np.array_equal(t.stack.x.float().numpy(), inputs[0]) and np.array_equal(t.dz.float().numpy(), inputs[1])
+    for l, p in enumerate(layers):
+        for k, v in p.items():
+            assert np.array_equal(t.params[f"{l}.{k}"].float().numpy(), v), k
+            if dtype == "bf16":
+                assert np.array_equal(t.masters[f"{l}.{k}"].numpy(), v), k
+    assert np.array_equal(t.params["norm_w"].float().numpy(), norm[0]) and np.array_equal(t.params["norm_b"].float().numpy(), norm[1])
+    assert int(t.step) == 0 and all(bool((v == 0).all()) for st in t.states.values() for v in st.values())
+
+
+def test_inputs_without_a_gradient_and_with_one_again(on_cpu):
+    t = _new("f32", "cpu")
+    x, dz = _values("f32", 0)[2]
+    t.set_inputs(x)
+    assert t.dz is None
+    t.set_inputs(x, dz)
+    at = t.dz.data_ptr()
+    t.set_inputs(x)
+    assert t.dz is None
+    t.set_inputs(x, dz)
+    assert t.dz.data_ptr() == at
 
 
 def test_values_that_do_not_fit_are_refused_and_change_nothing(on_cpu):
@@ -66,3 +118,60 @@ def test_values_that_do_not_fit_are_refused_and_change_nothing(on_cpu):
     for l, p in enumerate(layers):
         for k, v in p.items():
             assert np.array_equal(t.params[f"{l}.{k}"].numpy(), v), k
+
+
+# ---- on the GPU --------------------------------------------------------------------------------------------------------------------
+
+def _one(t, stream=None):
+    t.forward(stream)
+    t.backward(stream)
+    t.update(stream)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,bits", [("f32", 32), ("bf16", 8)])
+def test_a_captured_step_goes_on_with_new_values(dtype, bits):
+    """Replays after set_inputs and set_params are the steps of a trainer that has had these values from the start."""
+    from paper_2409_06206_amd import gswa
+    t = _new(dtype, state_bits=bits, flags=gswa.GSWA_DETERMINISTIC)
+    layers, norm, inputs = _values(dtype, 0)
+    t.set_params(layers, *norm)
+    t.set_inputs(*inputs)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        _one(t)
+    for n in (1, 2, 3):
+        layers, norm, inputs = _values(dtype, n)
+        other = _new(dtype, state_bits=bits, flags=gswa.GSWA_DETERMINISTIC)
+        for each in (t, other):
+            each.set_params(layers, *norm)
+            each.set_inputs(*inputs)
+        graph.replay()
+        _one(other)
+        torch.cuda.synchronize()
+        assert torch.equal(t.z, other.z) and int(t.step) == int(other.step) == 1
+        for k, g in other.grads.items():   # (part of them are summed by atomics)
+            assert float((t.grads[k].double() - g.double()).abs().max()) <= 1e-5 * float(g.double().abs().max()) + 1e-30, k
+
+
+@gpu
+def test_new_inputs_wait_for_a_step_that_reads_the_old_ones():
+    """Steps on a stream of their own, new inputs right behind each."""
+    t, waited = _new("f32"), _new("f32")
+    layers, norm, _ = _values("f32", 0)
+    stream, ends = torch.cuda.Stream(), []
+    for each in (t, waited):
+        each.set_params(layers, *norm)
+        zs = []
+        for n in range(6):
+            each.set_inputs(*_values("f32", n)[2])
+            each.forward(stream)
+            if each is waited:
+                torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                zs.append(each.z.clone())
+        torch.cuda.synchronize()
+        ends.append(zs)
+    for n, (a, b) in enumerate(zip(*ends)):
+        assert torch.equal(a, b), n
