@@ -183,13 +183,16 @@ class DeviceTrainer:
 
     ``edges``: the bias tables of the layers come from learned tables of buckets of offsets (see include/relpos.h); None: every row of
     a table is learned.  A step allocates nothing and reads nothing back, so it can be captured into a graph; ``set_params`` and ``set_inputs``
-    wait for the steps under way and put new values where the old ones were, so a captured step goes on with them."""
+    wait for the steps under way and put new values where the old ones were, so a captured step goes on with them.
+
+    ``skip_nonfinite``: an update whose gradients' norm is infinite or NaN changes nothing, the count of steps included; without it such a
+    gradient stays in parameters and states for good."""
 
     DECAYED = ("w_qkv", "w_proj", "w_fc1", "w_fc2")
 
     def __init__(self, B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every=0, eps=1e-5, flags=0,
                  device="cuda:0", dqk=0, edges=None, lr=2e-4, betas=(0.9, 0.999), adam_eps=1e-8, weight_decay=0.01, max_norm=1.0,
-                 state_bits=32, seed=0):
+                 state_bits=32, seed=0, skip_nonfinite=False):
         if flags & gswa.GSWA_ACCUM_WGRAD:
             raise ValueError("a step's gradients are its own: GSWA_ACCUM_WGRAD is not taken")
         self.stack = DeviceStack(B, H, W, C, heads, groups, window, shift, dtype, hidden, n_layers, checkpoint_every, eps, flags,
@@ -197,7 +200,7 @@ class DeviceTrainer:
         self.lr, self.weight_decay, self.max_norm = lr, weight_decay, max_norm
         self.norm_desc = lnorm.make_desc(B * H * W, C, dtype, eps)
         self.bias_desc = None if edges is None else relpos.make_desc(heads, edges, dtype, relpos.RELPOS_BIDIRECTIONAL, window=window)
-        self.adam_desc = adamw.make_desc(*betas, adam_eps, state_bits, seed=seed)
+        self.adam_desc = adamw.make_desc(*betas, adam_eps, state_bits, adamw.ADAMW_SKIP_NONFINITE if skip_nonfinite else 0, seed)
         new = lambda *shape, dtype=self.stack.y.dtype: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
         self.z, self.stack.dy = new(B, H, W, C), new(B, H, W, C)
         self._x, self._dz, self.dz = new(B, H, W, C), new(B, H, W, C), None

@@ -94,6 +94,12 @@ def test_inputs_without_a_gradient_and_with_one_again(on_cpu):
     assert t.dz.data_ptr() == at
 
 
+@pytest.mark.parametrize("skip", [False, True])
+def test_steps_that_are_not_finite_can_be_skipped(on_cpu, skip):
+    from paper_2409_06206_amd import adamw
+    assert _new("f32", "cpu", skip_nonfinite=skip).adam_desc.flags == (adamw.ADAMW_SKIP_NONFINITE if skip else 0)
+
+
 def test_values_that_do_not_fit_are_refused_and_change_nothing(on_cpu):
     t = _new("f32", "cpu")
     layers, norm, (x, dz) = _values("f32", 0)
@@ -175,3 +181,44 @@ def test_new_inputs_wait_for_a_step_that_reads_the_old_ones():
         ends.append(zs)
     for n, (a, b) in enumerate(zip(*ends)):
         assert torch.equal(a, b), n
+
+
+def _held(t):
+    """Everything that an update changes, copied."""
+    out = {"step": t.step, **{f"params.{k}": v for k, v in t.params.items()}, **{f"masters.{k}": v for k, v in t.masters.items()}}
+    out.update({f"states.{k}.{n}": v for k, st in t.states.items() for n, v in st.items()})
+    return {k: v.clone() for k, v in out.items()}
+
+
+@gpu
+@pytest.mark.parametrize("dtype,bits", [("f32", 32), ("bf16", 8)])
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+def test_gradients_that_are_not_finite_change_nothing(dtype, bits, bad):
+    """Eagerly and replayed; the step behind is the one it would have been."""
+    t = _new(dtype, state_bits=bits, skip_nonfinite=True)
+    layers, norm, (x, dz) = _values(dtype, 0)
+    t.set_params(layers, *norm)
+    t.set_inputs(x, dz)
+    _one(t)
+    torch.cuda.synchronize()
+    assert int(t.step) == 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _one(t)
+    broken = dz.copy()
+    broken[1, 3, 5, 7] = bad
+    t.set_inputs(x, broken)
+    before = _held(t)
+    for step in (lambda: _one(t), graph.replay, graph.replay):
+        step()
+        torch.cuda.synchronize()
+        assert not np.isfinite(float(t.grad_norm))
+        for k, v in _held(t).items():
+            assert torch.equal(v, before[k]), k
+    t.set_inputs(x, dz)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(t.step) == 2 and np.isfinite(float(t.grad_norm))
+    after = _held(t)
+    assert all(not torch.equal(after[f"params.{k}"], before[f"params.{k}"]) for k in t.params)
+    assert all(bool(torch.isfinite(v.float()).all()) for v in after.values())
