@@ -186,7 +186,8 @@ class DeviceTrainer:
     wait for the steps under way and put new values where the old ones were, so a captured step goes on with them.
 
     ``skip_nonfinite``: an update whose gradients' norm is infinite or NaN changes nothing, the count of steps included; without it such a
-    gradient stays in parameters and states for good."""
+    gradient stays in parameters and states for good.  ``lr_scale``, a value on the device, multiplies the learning rate: a schedule for steps that
+    are captured, whose ``lr`` is that of their capture."""
 
     DECAYED = ("w_qkv", "w_proj", "w_fc1", "w_fc2")
 
@@ -213,6 +214,7 @@ class DeviceTrainer:
         self.bias_ws = None if edges is None else new(relpos.relpos_query_bytes(self.bias_desc) + 256, dtype=torch.uint8)
         self.step = torch.zeros(1, dtype=torch.int64, device=device)
         self.grad_norm = torch.zeros((), device=device)
+        self.lr_scale = torch.ones((), device=device)
         self.params = self.masters = self.states = self.plan = self.plan_buffer = None
 
     def set_params(self, per_layer, norm_w, norm_b):
@@ -300,4 +302,4 @@ class DeviceTrainer:
 
     def update(self, stream=None):
         adamw.adamw_norm(self.plan, self.grad_norm, stream)
-        adamw.adamw_step(self.plan, self.step, self.lr, norm=self.grad_norm, max_norm=self.max_norm, stream=stream)
+        adamw.adamw_step(self.plan, self.step, self.lr, self.lr_scale, self.grad_norm, self.max_norm, stream)

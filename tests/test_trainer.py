@@ -222,3 +222,32 @@ def test_gradients_that_are_not_finite_change_nothing(dtype, bits, bad):
     after = _held(t)
     assert all(not torch.equal(after[f"params.{k}"], before[f"params.{k}"]) for k in t.params)
     assert all(bool(torch.isfinite(v.float()).all()) for v in after.values())
+
+
+@gpu
+def test_the_learning_rate_of_captured_steps():
+    """lr_scale of a replayed update is read when it runs: 0 moves nothing, a power of two is the same bits as that learning rate."""
+    layers, norm, (x, dz) = _values("f32", 0)
+    t, other = _new("f32"), _new("f32")
+    for each in (t, other):
+        each.set_params(layers, *norm)
+        each.set_inputs(x, dz)
+    t.forward()
+    t.backward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t.update()
+    for k, g in t.grads.items():
+        other.grads[k].copy_(g)
+    for n, scale in enumerate((0.0, 1.0, 0.5, 0.25)):
+        before = _held(t)
+        t.lr_scale.fill_(scale)
+        graph.replay()
+        other.lr = 1e-2 * scale
+        other.update()
+        torch.cuda.synchronize()
+        a, b = _held(t), _held(other)
+        for k, v in a.items():
+            assert torch.equal(v, b[k]), (n, k)
+        assert all(torch.equal(a[f"params.{k}"], before[f"params.{k}"]) == (scale == 0) for k in t.params)
