@@ -1,4 +1,7 @@
-"""runner.DeviceTrainer beside the step itself (tests/test_training_step.py): what its buffers do between steps and what it refuses.
+"""runner.DeviceTrainer beside the step itself (tests/test_training_step.py): what its buffers do between steps, its update
+over several steps and by a graph, and what it refuses.
+
+The update has the tolerances of the operator's own tests (tests/test_adamw.py).
 """
 import numpy as np
 import pytest
@@ -251,3 +254,54 @@ def test_the_learning_rate_of_captured_steps():
         for k, v in a.items():
             assert torch.equal(v, b[k]), (n, k)
         assert all(torch.equal(a[f"params.{k}"], before[f"params.{k}"]) == (scale == 0) for k in t.params)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,bits", [("f32", 32), ("f32", 8), ("bf16", 32), ("bf16", 8)])
+def test_updates_of_several_steps(dtype, bits):
+    """Parameters, fp32 copies and states of three steps from zero states on, each from what the one before left."""
+    from tests.test_adamw import U, _check_step, _cpu
+    t = _new(dtype, state_bits=bits)
+    layers, norm, _ = _values(dtype, 0)
+    t.set_params(layers, *norm)
+    flat = lambda: [{k: v.reshape(-1) if torch.is_tensor(v) else v for k, v in part.items()} for part in _cpu(t.plan.tensors)]  # noqa: E731
+    for n in range(3):
+        t.set_inputs(*_values(dtype, n)[2])
+        t.forward()
+        t.backward()
+        before = flat()
+        t.update()
+        after = flat()
+        want = float(torch.sqrt(sum(b["g"].double().square().sum() for b in before)))
+        assert abs(float(t.grad_norm) - want) <= 2 * U * want and want > 0.5 and int(t.step) == n + 1
+        _check_step(before, after, t.adam_desc, n + 1, 1e-2, 0.5 / want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,bits", [("f32", 32), ("f32", 8), ("bf16", 32), ("bf16", 8)])
+def test_replayed_updates_are_the_eager_ones(dtype, bits):
+    """Five updates in a row, eagerly and replayed, from the same gradients: the same bits of all that an update writes."""
+    eager, replayed = _new(dtype, state_bits=bits), _new(dtype, state_bits=bits)
+    layers, norm, _ = _values(dtype, 0)
+    for t in (eager, replayed):
+        t.set_params(layers, *norm)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        replayed.update()
+    for n in range(5):
+        eager.set_inputs(*_values(dtype, n)[2])
+        eager.forward()
+        eager.backward()
+        for k, g in eager.grads.items():
+            replayed.grads[k].copy_(g)
+        before = _held(replayed)
+        graph.replay()
+        eager.update()
+        torch.cuda.synchronize()
+        a, b = _held(eager), _held(replayed)
+        assert int(eager.step) == n + 1 and torch.equal(eager.grad_norm, replayed.grad_norm)
+        for k, v in a.items():
+            assert torch.equal(v, b[k]), (n, k)
+        for k in replayed.params:   # (and something was written)
+            assert not torch.equal(b[f"states.{k}.m"], before[f"states.{k}.m"]), (n, k)
