@@ -494,6 +494,7 @@ long ceil_div(long a, long b) { return (a + b - 1) / b; }
 int make_plan(const relpos_desc *d, Plan *p)
 {
     if (!d) return GSWA_EINVAL;
+    *p = Plan{}; // (the window form has no tiles)
     if (d->heads <= 0 || d->heads > 65535 || (d->dtype != GSWA_F32 && d->dtype != GSWA_BF16)) return GSWA_EINVAL;
     if (d->flags & ~(uint32_t)(RELPOS_BIDIRECTIONAL | RELPOS_CAUSAL | RELPOS_ACCUM_WGRAD)) return GSWA_EINVAL;
     if (d->n_edges < 0 || d->n_edges > RELPOS_MAX_EDGES || d->window < 0 || d->window > 64) return GSWA_EINVAL;
@@ -509,9 +510,6 @@ int make_plan(const relpos_desc *d, Plan *p)
         p->buckets = side * side;
         p->out = (size_t)offsets * d->heads * p->elem;
         p->dout = (size_t)offsets * d->heads * sizeof(float);
-        p->slices = 0;
-        p->ws = 0;
-        p->ld = 0;
     } else {
         if (d->batch <= 0 || d->q_len <= 0 || d->k_len <= 0 || d->q_start < 0) return GSWA_EINVAL;
         if ((long)d->q_start + d->q_len > (1L << 30) || d->k_len > (1 << 30)) return GSWA_EUNSUPPORTED;
