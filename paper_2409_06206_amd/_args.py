@@ -3,6 +3,9 @@
 A tensor of the wrong type, size or layout would be read out of its bounds by a kernel; raw addresses (integers) are the
 caller's own.  Work goes to the device the tensors lie on and, where no stream is named, to that device's current stream.
 """
+import ctypes
+import operator
+
 import torch
 
 from .gswa import GSWA_BF16, GSWA_F32, GSWA_OK, _check
@@ -16,6 +19,20 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 def torch_dtype(code):
     return TORCH_DTYPES.get(code, torch.bfloat16)   # (a code that is none is refused by the library)
+
+
+class Whole:
+    """The whole numbers of a structure: ctypes cuts off what a field cannot hold, and what is left may be another valid number."""
+
+    def __init__(self, kind):
+        self.names = tuple(n for n, t in kind._fields_ if t in (ctypes.c_int32, ctypes.c_uint32, ctypes.c_int64, ctypes.c_uint64))
+        self.of = operator.attrgetter(*self.names)
+
+    def held(self, made, *given):
+        """`made`, whose whole numbers have to be the `given` ones."""
+        if self.of(made) != given:
+            raise ValueError("; ".join(f"{n} cannot hold {v}" for n, v in zip(self.names, given) if getattr(made, n) != v))
+        return made
 
 
 class Specs(dict):

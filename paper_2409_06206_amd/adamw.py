@@ -9,7 +9,7 @@ import struct
 import torch
 
 from . import gswa
-from ._args import Call
+from ._args import Call, Whole
 from .gswa import GSWA_BF16, GSWA_F32, _check
 
 EXPORTS = ("adamw_query_bytes", "adamw_plan", "adamw_norm", "adamw_step", "adamw_unpack")
@@ -55,8 +55,12 @@ def lib():
     return L
 
 
+_whole = Whole(adamw_desc)
+
+
 def make_desc(beta1=0.9, beta2=0.999, eps=1e-8, state_bits=32, flags=0, seed=0):
-    return adamw_desc(beta1, beta2, eps, state_bits, flags, seed)
+    seed = int(seed) & 0xFFFFFFFFFFFFFFFF
+    return _whole.held(adamw_desc(beta1, beta2, eps, state_bits, flags, seed), state_bits, flags, seed)
 
 
 _FIELDS = frozenset(("p", "master", "g", "m", "v", "m_exp", "v_exp", "weight_decay"))

@@ -8,7 +8,7 @@ import ctypes
 import torch
 
 from . import gswa
-from ._args import DTYPES, Call, Specs, row_spec, torch_dtype
+from ._args import DTYPES, Call, Specs, Whole, row_spec, torch_dtype
 from .gswa import GSWA_OK, _check
 
 EXPORTS = ("lnorm_query_bytes", "lnorm_forward", "lnorm_backward")
@@ -39,8 +39,12 @@ def lib():
     return L
 
 
+_whole = Whole(lnorm_desc)
+
+
 def make_desc(rows, C, dtype, eps=1e-5, flags=0, x_stride=0, y_stride=0, r_stride=0):
-    return lnorm_desc(rows, C, DTYPES.get(dtype, dtype), eps, flags, x_stride, y_stride, r_stride)
+    code = DTYPES.get(dtype, dtype)
+    return _whole.held(lnorm_desc(rows, C, code, eps, flags, x_stride, y_stride, r_stride), rows, C, code, flags, x_stride, y_stride, r_stride)
 
 
 def lnorm_query_bytes(desc):

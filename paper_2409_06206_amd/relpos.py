@@ -8,7 +8,7 @@ import ctypes
 import torch
 
 from . import gswa
-from ._args import DTYPES, Call, Specs, row_spec, torch_dtype
+from ._args import DTYPES, Call, Specs, Whole, row_spec, torch_dtype
 from .gswa import GSWA_OK, _check
 
 EXPORTS = ("relpos_log_edges", "relpos_query_bytes", "relpos_forward", "relpos_backward")
@@ -51,16 +51,25 @@ def lib():
 def relpos_log_edges(buckets, max_distance, bidirectional):
     """List of edges: single distances first, then even steps of the logarithm up to max_distance."""
     n, edges = ctypes.c_int32(), (ctypes.c_int32 * RELPOS_MAX_EDGES)()
+    for v in (buckets, max_distance):
+        if ctypes.c_int32(v).value != v:
+            raise ValueError(f"32 bits cannot hold {v}")
     _check(lib().relpos_log_edges(buckets, max_distance, int(bool(bidirectional)), ctypes.byref(n), edges))
     return list(edges[: n.value])
+
+
+_whole = Whole(relpos_desc)
 
 
 def make_desc(heads, edges, dtype, flags=0, q_len=0, k_len=0, q_start=0, batch=1, window=0, row_stride=0):
     """Sequence form with q_len and k_len, window form with window."""
     if len(edges) > RELPOS_MAX_EDGES:
         raise ValueError(f"{len(edges)} edges, at most {RELPOS_MAX_EDGES}")
-    return relpos_desc(heads, DTYPES.get(dtype, dtype), flags, window, batch, q_len, k_len, q_start, row_stride, len(edges),
-                       (ctypes.c_int32 * RELPOS_MAX_EDGES)(*edges))
+    code, n, places = DTYPES.get(dtype, dtype), len(edges), (ctypes.c_int32 * RELPOS_MAX_EDGES)(*edges)
+    if places[:n] != list(edges):
+        raise ValueError(f"edges cannot hold {[e for e, p in zip(edges, places) if e != p]}")
+    return _whole.held(relpos_desc(heads, code, flags, window, batch, q_len, k_len, q_start, row_stride, n, places),
+                       heads, code, flags, window, batch, q_len, k_len, q_start, row_stride, n)
 
 
 def relpos_query_bytes(desc):

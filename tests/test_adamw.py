@@ -30,6 +30,16 @@ def test_exports():
         assert hasattr(adamw.lib(), n)
 
 
+@pytest.mark.parametrize("change", [dict(state_bits=(1 << 32) + 8), dict(flags=1 << 32)])
+def test_numbers_that_a_field_cannot_hold_are_refused(change):
+    with pytest.raises(ValueError, match="hold"):
+        adamw.make_desc(**change)
+
+
+def test_seeds_are_taken_modulo_2_to_64():
+    assert adamw.make_desc(seed=-1).seed == adamw.make_desc(seed=(1 << 64) - 1).seed == adamw.make_desc(seed=(1 << 65) - 1).seed == (1 << 64) - 1
+
+
 def _c_tensors(*parts):
     out = (adamw.adamw_tensor * len(parts))()
     for i, p in enumerate(parts):

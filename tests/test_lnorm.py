@@ -44,6 +44,13 @@ def test_bad_descriptors(change, status):
     assert e.value.status == status
 
 
+@pytest.mark.parametrize("change", [dict(rows=1 << 64), dict(C=(1 << 32) + 60), dict(x_stride=(1 << 64) + 60), dict(flags=1 << 32), dict(dtype=1 << 32)])
+def test_numbers_that_a_field_cannot_hold_are_refused(change):
+    """Cut off to 32 or 64 bits they would be other, valid ones."""
+    with pytest.raises(ValueError, match="hold"):
+        lnorm.make_desc(**{**dict(rows=4, C=60, dtype="bf16"), **change})
+
+
 def test_scratch_is_a_multiple_of_256():
     for rows, C in ((1, 1), (7, 60), (131072, 180), (4096, 16384)):
         n = lnorm.lnorm_query_bytes(lnorm.make_desc(rows, C, "bf16"))

@@ -65,6 +65,17 @@ def test_too_many_edges():
         relpos.make_desc(1, list(range(1, 129)), "f32", q_len=1, k_len=1)
 
 
+@pytest.mark.parametrize("change", [dict(q_start=(1 << 32) + 5), dict(heads=(1 << 32) + 4), dict(edges=[1, (1 << 32) + 4]), dict(batch=1 << 32),
+                                    dict(row_stride=(1 << 64) + 7), dict(window=-(1 << 32) + 8)])
+def test_numbers_that_a_field_cannot_hold_are_refused(change):
+    """Cut off to 32 or 64 bits they would be other, valid ones."""
+    with pytest.raises(ValueError, match="hold"):
+        relpos.make_desc(**{**GOOD, **change})
+    for buckets, distance in ((32, (1 << 32) + 128), ((1 << 32) + 32, 128), (32, 1 << 31)):
+        with pytest.raises(ValueError, match="hold"):
+            relpos.relpos_log_edges(buckets, distance, True)
+
+
 def test_bad_buffers_are_refused_before_a_launch():
     d = relpos.make_desc(**GOOD)
     size = relpos.relpos_query_bytes(d)
