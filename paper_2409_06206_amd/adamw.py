@@ -125,7 +125,10 @@ def adamw_query_bytes(desc, tensors):
 
 
 def adamw_plan(desc, tensors, buffer, stream=None):
-    """The Plan that the calls below take; it keeps the tensors and the buffer alive."""
+    """The Plan that the calls below take; it keeps the tensors and the buffer alive.
+
+    Checking and listing the tensors here takes some 2 us each (468 of them 1.1 ms, where norm and step take 16 us): a plan is made once for tensors
+    that stay where they are, gradients too.  A program whose gradients are allocated anew each step would pay for it each step."""
     L, n = lib(), ctypes.c_size_t()
     listed, device = _list(desc, tensors)
     c = Call(device)

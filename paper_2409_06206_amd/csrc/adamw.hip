@@ -23,9 +23,10 @@ constexpr int kStepBlocks = 65536;      // and of the others: a workgroup a piec
 constexpr int kGroups = 32;             // of the workgroups that are counted together (see last_of_all)
 constexpr int kCounterStep = 32;        // counters stand in lines of their own
 
-// Blocks of a piece of work that a wavefront takes at once.  Four for large lists, whose loads then keep the memory busy (201 M elements, 8-bit states: a step
-// 598 us and the read-back 218, with two blocks 672 and 308).  One for lists that do not fill the card, where the time of one wavefront counts (13 tensors
-// of a layer, 23 K elements: a step 5.6 us, with four 7.0; 0.9 M elements in 468 tensors: 9.9 us, with four 11).
+// Blocks of a piece of work that a wavefront takes at once.  Four for large lists, whose loads then keep the memory busy (201 M elements, steps one after another:
+// fp32 states 1042 us, with two blocks 1075; 8-bit states and bf16 alone 458 and 482, the read-back 197 and 262; beside an fp32 copy 589 and 591; 7.7 M
+// elements in 8 bits the same either way, 26).  One for lists that do not fill the card, where the time of one wavefront counts (8-bit states, 13 tensors of a
+// layer, 25 K elements: 5.4 us, with four 7.1; 0.9 M elements in 468 tensors: 8.5, with four 9.7).
 constexpr int kMany = 4;
 constexpr long kSmall = 8192;           // blocks of a list that does not: up to 2 M elements, 8 workgroups a compute unit
 constexpr long chunk_of(int each) { return (long)kBlock * kWaves * each; }
@@ -438,7 +439,7 @@ template <int N, typename F, typename H> __device__ __forceinline__ void each_bl
         if (b * kBlock < T.n) partly(b);
 }
 
-// Bound by memory, but with 8-bit states and no fp32 copy: 10 to 30 bytes an element against 70 operations with 8-bit states, half of that with 32.  A wavefront has all loads of
+// Bound by memory, but with 8-bit states and no fp32 copy: 10 to 30 bytes an element against 75 operations with 8-bit states, half of that with 32.  A wavefront has all loads of
 // N blocks in flight together; a block's largest magnitude comes from exchanges between its lanes.
 template <bool EIGHT, int N> __global__ __launch_bounds__(kThreads) void step_kernel(Step a)
 {

@@ -166,7 +166,7 @@ enum {
 //           as apart 4.3; rows of 4032 5.4)
 //   apart   back to the line that the row starts in; elements before the first aligned vector and behind the last one are stored one by one, by a lane
 //           each, of all rows at once
-//   single  as apart, by the lanes that have them in a vector (one token against 8190 keys: 4.8 us, as apart 5.9)
+//   single  as apart, by the lanes that have them in a vector (one token against 8190 keys: 5.3 us, as apart 6.4)
 template <typename T, int THREADS, int ROWS> __global__ __launch_bounds__(THREADS) void sequence_fwd_kernel(Args a)
 {
     typedef Vector<T> Vec;
