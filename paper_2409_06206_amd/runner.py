@@ -227,8 +227,8 @@ class DeviceTrainer:
         if set(named) != set(self.grads):
             raise ValueError(f"parameters missing: {sorted(set(self.grads) - set(named))}, unknown: {sorted(set(named) - set(self.grads))}")
         for k, v in named.items():
-            if np.size(v) != self.grads[k].numel():
-                raise ValueError(f"{k} has {np.size(v)} values, {self.grads[k].numel()} are needed")
+            if np.asarray(v).size != self.grads[k].numel():
+                raise ValueError(f"{k} has {np.asarray(v).size} values, {self.grads[k].numel()} are needed")
         if self.params is None:
             self._allocate(named, len(per_layer))
         self._settle()
@@ -275,8 +275,8 @@ class DeviceTrainer:
         """Without dz there is nothing for ``backward`` to start from."""
         s, shape = self.stack, self.z.shape
         for a in (x, dz):
-            if a is not None and np.size(a) != self.z.numel():
-                raise ValueError(f"{np.size(a)} values, {tuple(shape)} are needed")
+            if a is not None and np.asarray(a).size != self.z.numel():
+                raise ValueError(f"{np.asarray(a).size} values, {tuple(shape)} are needed")
         self._settle()
         s.x, self.dz = self._x, None if dz is None else self._dz
         for t, a in ((s.x, x), (self.dz, dz)):

@@ -97,6 +97,20 @@ def test_inputs_without_a_gradient_and_with_one_again(on_cpu):
     assert t.dz.data_ptr() == at
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_in_other_containers(on_cpu, dtype):
+    """Tensors and flat arrays of the same values, as the layers' own classes take them."""
+    layers, norm, (x, dz) = _values(dtype, 0)
+    t, other = _new(dtype, "cpu"), _new(dtype, "cpu")
+    t.set_params(layers, *norm)
+    t.set_inputs(x, dz)
+    other.set_params([{k: torch.from_numpy(v) for k, v in p.items()} for p in layers], torch.from_numpy(norm[0]), norm[1].tolist())
+    other.set_inputs(torch.from_numpy(x), dz.reshape(-1))
+    assert torch.equal(t.stack.x, other.stack.x) and torch.equal(t.dz, other.dz)
+    for k, v in t.params.items():
+        assert torch.equal(v, other.params[k]), k
+
+
 @pytest.mark.parametrize("skip", [False, True])
 def test_steps_that_are_not_finite_can_be_skipped(on_cpu, skip):
     from paper_2409_06206_amd import adamw
